@@ -389,6 +389,138 @@ int sw_decode_step(int dtype, int layers, int batch, int h_q, int h_kv, int d, i
                    uint32_t flags, int kmax, float scale, double* rows, int32_t* idx, int32_t* cnt,
                    void* O, void* workspace, int64_t workspace_bytes, void* stream);
 
+/* ======================================================================
+ * Paged 8-bit key/value cache: pages handed out on the GPU from the requests'
+ * lengths, tokens written and read back, decode attention over it.
+ *
+ * One layer's pool of n_pages pages (device):
+ *   k_pages [n_pages][h_kv][B][d], v_pages [n_pages][h_kv][d][B]  e4m3 codes,
+ *     one byte each (the values' pages are transposed)
+ *   k_scale, v_scale [n_pages][h_kv]  exponent + 127 of the power of two by
+ *     which every code of a (page, head) is multiplied, in [1, 254]
+ * A page holds one key block of B tokens, the unit of selection. The scale is
+ * the smallest power of two (at least 2^-126) with which no value exceeds 448,
+ * the largest code; a code is x / scale rounded to nearest even, so a stored
+ * value is off by at most 2^-4 of itself, or 2^-10 of the scale below 2^-6 of
+ * it. A value that is not finite is stored as NaN and does not count for the
+ * scale. Layers are stacked: pages and scales of layer l follow those of layer
+ * l - 1, and share one block table.
+ *
+ * Block table of a sequence: tables [n_seqs][b_max] int32, the page of each of
+ * its blocks. An entry outside [0, n_pages) is no page: nothing is written
+ * there, and attention skips the block. A page belongs to one sequence as long
+ * as that is written to.
+ *
+ * d in {64, 128}; B a multiple of 16 in [16, 1024]; n_pages * B < 2^31.
+ * ====================================================================== */
+
+#define SW_MAX_APPEND_TOKENS 4096 /* tokens of an append without cu_seqlens */
+
+/*
+ * sw_block_tables - brings the block tables of n_seqs requests from their old
+ * lengths to their new ones (tokens; 0: no request) in one call.
+ *
+ * Blocks ceil(new / B) .. ceil(old / B) - 1 of a request that shrinks or ends go
+ * back to the pool, in ascending order of request and block, the first of them
+ * on top of the stack of free pages; their entries become -1. Blocks
+ * ceil(old / B) .. ceil(new / B) - 1 of one that enters or grows then take the
+ * pages on top, in the same order. Taking a step back therefore restores
+ * tables and stack as they were.
+ *
+ *   old_len, new_len [n_seqs] int32       tables [n_seqs][b_max] int32, updated
+ *   free_pages [n_pages] int32, n_free [1] int32: the stack and its height,
+ *     updated (entries above the height are scratch)
+ *   slots [n_slots] int32 (out): page * B + place of every new token, requests in
+ *     order. rows = 0: packed, -1 behind the last. rows > 0: rows entries per
+ *     request (n_slots = n_seqs * rows), -1 behind its new tokens.
+ *   cu_seqlens [n_seqs + 1] int32 (out): cumulative numbers of new tokens
+ *   pos [n_seqs] int32 (out): position of the last token, new_len - 1
+ *   status [1] int32 (out): 0; 1: too few free pages; 2: a length outside
+ *     [0, b_max * B], more new tokens than slots or than rows, or more pages
+ *     given back than the pool has. With 1 and 2 nothing changes, cu_seqlens is
+ *     0, every slot -1 and pos old_len - 1.
+ * The buffers must not overlap.
+ */
+int sw_block_tables(int n_seqs, int B, int b_max, const int32_t* old_len, const int32_t* new_len,
+                    int32_t* tables, int32_t* free_pages, int32_t* n_free, int n_pages, int rows,
+                    int64_t n_slots, int32_t* slots, int32_t* cu_seqlens, int32_t* pos,
+                    int32_t* status, void* stream);
+
+/*
+ * sw_kv_append_q8 - writes N tokens' keys and values into the pages that their
+ * slots (as from sw_block_tables) name; a negative slot, or one behind the
+ * pool, is skipped. Element e of head h of token i is k[h * k_head_stride + i *
+ * k_token_stride + e] (strides in elements, whole 16-byte pieces, not negative).
+ *
+ * A page whose first place is among the call's tokens is begun: its scales are
+ * those of the new tokens alone. Another keeps its scales unless a new token
+ * needs a larger one; then its codes are rounded again to that.
+ *
+ * cu_seqlens [n_seqs + 1] int32 (device): the tokens of a sequence lie together
+ * and fill its pages one place after the other, from the first token's slot on;
+ * a sequence whose first slot is negative is skipped. NULL (n_seqs unused):
+ * any order, at most SW_MAX_APPEND_TOKENS tokens; of two tokens with one slot
+ * the later one stays.
+ */
+int sw_kv_append_q8(int dtype, const void* k, const void* v, int64_t k_head_stride,
+                    int64_t k_token_stride, int64_t v_head_stride, int64_t v_token_stride, int64_t N,
+                    int n_seqs, const int32_t* cu_seqlens, const int32_t* slots, int n_pages,
+                    int h_kv, int d, int B, void* k_pages, void* v_pages, uint8_t* k_scale,
+                    uint8_t* v_scale, void* stream);
+
+/*
+ * sw_kv_fetch_q8 - reads tokens back as keys and values of `dtype`: positions
+ * first[s] .. of sequence s into rows cu_seqlens[s] .. cu_seqlens[s+1] - 1 of K
+ * and V [h_kv][N][d], the layout that sw_sparse_attn_prefill and
+ * sw_sketch_scores take (a cached prefix before a longer prompt). The values are
+ * exact. first [n_seqs] int32 may be NULL (0), cu_seqlens int32: both device.
+ * A position without a page reads as zero; rows behind the last sequence are
+ * left as they were.
+ */
+int sw_kv_fetch_q8(int dtype, const void* k_pages, const void* v_pages, const uint8_t* k_scale,
+                   const uint8_t* v_scale, int n_pages, int h_kv, int d, int B, int n_seqs, int b_max,
+                   const int32_t* tables, const int32_t* first, const int32_t* cu_seqlens, int64_t N,
+                   void* K, void* V, void* stream);
+
+/* Host-only: workspace bytes of sw_sparse_attn_decode_q8 (-1 on bad input). */
+int64_t sw_decode_attn_q8_workspace_bytes(int batch, int h_q, int h_kv, int d);
+
+/*
+ * sw_sparse_attn_decode_q8 - sw_sparse_attn_decode over the paged 8-bit cache:
+ * the same attention with the keys and values that the codes stand for. Blocks
+ * idx[b][0..cnt[b]) of sequence b lie in pages tables[b][idx]; tokens behind
+ * pos[b] do not count whatever their places hold. Sequences with pos[b] outside
+ * [0, b_max * B), and those none of whose selected blocks has a page, get zeros.
+ * dtype (q, O) SW_BF16 or SW_F32; h_q / h_kv in [1, 16]; any kmax. fp32 takes q
+ * and the weights to 24 bits.
+ */
+int sw_sparse_attn_decode_q8(int dtype, const void* q, const void* k_pages, const void* v_pages,
+                             const uint8_t* k_scale, const uint8_t* v_scale, int batch, int h_q,
+                             int h_kv, int d, int n_pages, const int32_t* tables, int b_max, int B,
+                             const int32_t* pos, const int32_t* idx, const int32_t* cnt, int kmax,
+                             float scale, void* O, void* workspace, int64_t workspace_bytes,
+                             void* stream);
+
+/*
+ * sw_decode_step_q8 - sw_decode_step over the paged 8-bit cache: the new tokens
+ * go to `slots` [batch] (as from sw_block_tables with rows = 1; negative: none),
+ * the attention reads through tables [batch][b_max]. Pools are stacked over the
+ * layers. workspace: >= sw_decode_attn_q8_workspace_bytes(...) bytes, 256-byte
+ * aligned; with sw_decode_step_q8_workspace_bytes(...) several layers share an
+ * attention launch. batch at most SW_MAX_APPEND_TOKENS. The sketch, the walk and
+ * the selection are those of sw_decode_step, on the tokens as given; results are
+ * bit-identical to the per-layer calls.
+ */
+int64_t sw_decode_step_q8_workspace_bytes(int batch, int h_q, int h_kv, int d);
+int sw_decode_step_q8(int dtype, int layers, int batch, int h_q, int h_kv, int d, int r, int n_pages,
+                      int B, int b_max, const void* q_new, const void* k_new, const void* v_new,
+                      void* k_pages, void* v_pages, uint8_t* k_scale, uint8_t* v_scale,
+                      const int32_t* tables, const int32_t* slots, void* state, const int32_t* pos,
+                      const int8_t* signs, const int32_t* cols, int s, int walk_variant, int k,
+                      int density_pct, uint32_t flags, int kmax, float scale, double* rows,
+                      int32_t* idx, int32_t* cnt, void* O, void* workspace, int64_t workspace_bytes,
+                      void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -8,6 +8,7 @@ built or cannot be loaded, every call raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional, Sequence, Tuple
@@ -79,9 +80,25 @@ _SIGNATURES = {
     "sw_sparse_attn_decode_noalloc": (_c_int, [_c_int, _vp, _vp, _vp, _c_int, _c_int, _c_int, _c_int,
                                                _c_int, _c_int, _vp, _vp, _vp, _c_int, ctypes.c_float,
                                                _vp, _vp]),
+    "sw_block_tables": (_c_int, [_c_int, _c_int, _c_int, _vp, _vp, _vp, _vp, _vp, _c_int, _c_int,
+                                 _c_i64, _vp, _vp, _vp, _vp, _vp]),
+    "sw_kv_append_q8": (_c_int, [_c_int, _vp, _vp, _c_i64, _c_i64, _c_i64, _c_i64, _c_i64, _c_int, _vp,
+                                 _vp, _c_int, _c_int, _c_int, _c_int, _vp, _vp, _vp, _vp, _vp]),
+    "sw_kv_fetch_q8": (_c_int, [_c_int, _vp, _vp, _vp, _vp, _c_int, _c_int, _c_int, _c_int, _c_int,
+                                _c_int, _vp, _vp, _vp, _c_i64, _vp, _vp, _vp]),
+    "sw_decode_attn_q8_workspace_bytes": (_c_i64, [_c_int, _c_int, _c_int, _c_int]),
+    "sw_sparse_attn_decode_q8": (_c_int, [_c_int, _vp, _vp, _vp, _vp, _vp, _c_int, _c_int, _c_int,
+                                          _c_int, _c_int, _vp, _c_int, _c_int, _vp, _vp, _vp, _c_int,
+                                          ctypes.c_float, _vp, _vp, _c_i64, _vp]),
+    "sw_decode_step_q8_workspace_bytes": (_c_i64, [_c_int, _c_int, _c_int, _c_int]),
+    "sw_decode_step_q8": (_c_int, [_c_int, _c_int, _c_int, _c_int, _c_int, _c_int, _c_int, _c_int,
+                                   _c_int, _c_int, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+                                   _vp, _vp, _vp, _c_int, _c_int, _c_int, _c_int, ctypes.c_uint32,
+                                   _c_int, ctypes.c_float, _vp, _vp, _vp, _vp, _vp, _c_i64, _vp]),
 }
 
 NOALLOC_SCRATCH_BYTES = 8 * 1024 * 1024
+MAX_APPEND_TOKENS = 4096
 
 _lib = None
 
@@ -515,4 +532,228 @@ def decode_step(q_new: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, K
         _dev(o["O"], "O", q_new.dtype), _dev(workspace, "workspace"), workspace.numel(),
         _stream(dev))
     _check(rc, "sw_decode_step")
+    return o
+
+
+# ---------------------------------------------------------------------------
+# paged 8-bit cache
+# ---------------------------------------------------------------------------
+
+E4M3 = torch.float8_e4m3fn
+
+
+def new_cache_q8(n_pages: int, h_kv: int, B: int, d: int, device, layers: Optional[int] = None) -> dict:
+    """A zero-filled paged 8-bit cache of one layer, or of ``layers`` stacked ones:
+    k [n_pages][h_kv][B][d] and v [n_pages][h_kv][d][B] (e4m3), k_scale and v_scale
+    [n_pages][h_kv] (uint8, exponent + 127)."""
+    lead = () if layers is None else (layers,)
+
+    def zeros(shape, dtype):
+        return torch.zeros(lead + shape, dtype=torch.uint8, device=device).view(dtype)
+
+    return {"k": zeros((n_pages, h_kv, B, d), E4M3), "v": zeros((n_pages, h_kv, d, B), E4M3),
+            "k_scale": zeros((n_pages, h_kv), torch.uint8), "v_scale": zeros((n_pages, h_kv), torch.uint8)}
+
+
+def _same_device(dev: torch.device, *tensors: Optional[torch.Tensor]) -> None:
+    for t in tensors:
+        if t is not None and t.device != dev:
+            raise SketchWalkError(f"all tensors must be on {dev}, got {t.device}")
+
+
+_HERE_ALREADY = contextlib.nullcontext()
+
+
+def _on(dev: torch.device):
+    """Makes ``dev`` the current device where it is not (the launch goes to the current one)."""
+    if dev.type != "cuda":
+        raise SketchWalkError(f"tensors must be on a CUDA (HIP) device, got {dev}")
+    return _HERE_ALREADY if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
+
+
+def _pool(cache: dict, layers: Optional[int] = None):
+    """(n_pages, h_kv, B, d, pointers) of a cache as new_cache_q8 makes it."""
+    k, v, ks, vs = cache["k"], cache["v"], cache["k_scale"], cache["v_scale"]
+    lead = () if layers is None else (layers,)
+    if k.dim() != 4 + len(lead) or k.shape[:len(lead)] != lead:
+        raise SketchWalkError(f"cache k of shape {tuple(k.shape)}: {lead + ('n_pages', 'h_kv', 'B', 'd')} needed")
+    n_pages, h_kv, B, d = k.shape[-4:]
+    if v.shape != lead + (n_pages, h_kv, d, B):
+        raise SketchWalkError(f"cache v of shape {tuple(v.shape)} beside k of shape {tuple(k.shape)}")
+    for name, t in (("k_scale", ks), ("v_scale", vs)):
+        if t.shape != lead + (n_pages, h_kv):
+            raise SketchWalkError(f"cache {name} of shape {tuple(t.shape)} beside k of shape {tuple(k.shape)}")
+    _same_device(k.device, v, ks, vs)
+    return n_pages, h_kv, B, d, (_dev(k, "cache k", E4M3), _dev(v, "cache v", E4M3),
+                                 _dev(ks, "cache k_scale", torch.uint8), _dev(vs, "cache v_scale", torch.uint8))
+
+
+def _vec(t: torch.Tensor, n: int, name: str) -> int:
+    """A device int32 vector of n entries."""
+    p = _dev(t, name, torch.int32)
+    if t.numel() != n:
+        raise SketchWalkError(f"{name} has {t.numel()} entries, {n} needed")
+    return p
+
+
+def _mat(t: torch.Tensor, shape: tuple, name: str, dtype: torch.dtype = torch.int32) -> int:
+    p = _dev(t, name, dtype)
+    if tuple(t.shape) != shape:
+        raise SketchWalkError(f"{name} of shape {tuple(t.shape)}, {shape} needed")
+    return p
+
+
+def block_tables(old_len: torch.Tensor, new_len: torch.Tensor, B: int, tables: torch.Tensor,
+                 free_pages: torch.Tensor, n_free: torch.Tensor, n_slots: int, rows: int = 0,
+                 out: Optional[dict] = None) -> dict:
+    """Brings ``tables`` [n][b_max] from the requests' old lengths to the new ones,
+    with the stack of free pages (``free_pages`` [n_pages], its height ``n_free`` [1]);
+    all int32, the last three updated in place. Returns dict with slots [n_slots],
+    cu [n + 1], pos [n] and status [1] (0: done; otherwise nothing changed)."""
+    dev = tables.device
+    n, b_max = tables.shape
+    o = dict(out or {})
+    _fill(o, {"slots": (n_slots,), "cu": (n + 1,), "pos": (n,), "status": (1,)}, torch.int32, dev)
+    _same_device(dev, old_len, new_len, free_pages, n_free, *o.values())
+    with _on(dev):
+        rc = load().sw_block_tables(n, B, b_max, _vec(old_len, n, "old_len"), _vec(new_len, n, "new_len"),
+                                    _dev(tables, "tables", torch.int32),
+                                    _dev(free_pages, "free_pages", torch.int32), _vec(n_free, 1, "n_free"),
+                                    free_pages.numel(), rows, n_slots, _vec(o["slots"], n_slots, "slots"),
+                                    _vec(o["cu"], n + 1, "cu"), _vec(o["pos"], n, "pos"),
+                                    _vec(o["status"], 1, "status"), _stream(dev))
+    _check(rc, "sw_block_tables")
+    return o
+
+
+def kv_append_q8(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache: dict,
+                 cu: Optional[torch.Tensor] = None) -> None:
+    """Writes k, v [h_kv][N][d] (bf16 or fp32; heads and tokens in any strides of whole
+    16-byte pieces) into the pages of ``slots`` [N]. ``cu`` [n + 1] int32 (device): the
+    tokens of a sequence together, in order; without it at most MAX_APPEND_TOKENS."""
+    n_pages, h_kv, B, d, pages = _pool(cache)
+    dev = cache["k"].device
+    _same_device(dev, k, v, slots, cu)
+    for name, t in (("k", k), ("v", v)):
+        if not t.is_cuda:
+            raise SketchWalkError(f"{name} must be a CUDA (HIP) tensor")
+        if t.dim() != 3 or t.shape[0] != h_kv or t.shape[2] != d or t.shape != k.shape:
+            raise SketchWalkError(f"{name} of shape {tuple(t.shape)}, ({h_kv}, N, {d}) needed")
+        if t.stride(2) != 1:
+            raise SketchWalkError(f"{name} must be contiguous in its last dimension")
+    if k.dtype != v.dtype:
+        raise SketchWalkError("k and v must share a dtype")
+    N = k.shape[1]
+    n = 0 if cu is None else cu.numel() - 1
+    with _on(dev):
+        rc = load().sw_kv_append_q8(_dtype_code(k), k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1),
+                                    v.stride(0), v.stride(1), N, n, _opt(cu, "cu", torch.int32),
+                                    _vec(slots, N, "slots"), n_pages, h_kv, d, B, *pages, _stream(dev))
+    _check(rc, "sw_kv_append_q8")
+
+
+def kv_fetch_q8(cache: dict, tables: torch.Tensor, first: Optional[torch.Tensor], cu: torch.Tensor, N: int,
+                dtype: torch.dtype = torch.bfloat16, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None):
+    """K, V [h_kv][N][d] in ``dtype``: positions first[s] .. (``first`` None: 0) of sequence
+    s in rows cu[s] .. cu[s + 1] - 1 (device int32). Rows behind cu[n] are not written."""
+    n_pages, h_kv, B, d, pages = _pool(cache)
+    dev = cache["k"].device
+    n, b_max = tables.shape
+    if out is None:
+        out = tuple(torch.empty((h_kv, N, d), dtype=dtype, device=dev) for _ in range(2))
+    K, V = out
+    for name, t in (("K", K), ("V", V)):
+        if tuple(t.shape) != (h_kv, N, d):
+            raise SketchWalkError(f"{name} of shape {tuple(t.shape)}, ({h_kv}, {N}, {d}) needed")
+    _same_device(dev, tables, first, cu, K, V)
+    with _on(dev):
+        rc = load().sw_kv_fetch_q8(_dtype_code(K), *pages, n_pages, h_kv, d, B, n, b_max,
+                                   _dev(tables, "tables", torch.int32),
+                                   None if first is None else _vec(first, n, "first"),
+                                   _vec(cu, n + 1, "cu"), N, _dev(K, "K"), _dev(V, "V", K.dtype),
+                                   _stream(dev))
+    _check(rc, "sw_kv_fetch_q8")
+    return K, V
+
+
+def decode_attn_q8_workspace_bytes(batch: int, h_q: int, h_kv: int, d: int) -> int:
+    v = load().sw_decode_attn_q8_workspace_bytes(batch, h_q, h_kv, d)
+    if v < 0:
+        _check(1, "sw_decode_attn_q8_workspace_bytes")
+    return int(v)
+
+
+def sparse_attn_decode_q8(q: torch.Tensor, cache: dict, tables: torch.Tensor, pos: torch.Tensor,
+                          idx: torch.Tensor, cnt: torch.Tensor, kmax: int, scale: float = 0.0,
+                          O: Optional[torch.Tensor] = None,
+                          workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """sparse_attn_decode over a paged 8-bit cache: q [batch][h_q][d], tables
+    [batch][b_max], idx [batch][kmax]."""
+    n_pages, h_kv, B, d, pages = _pool(cache)
+    batch, h_q, dq = q.shape
+    if dq != d:
+        raise SketchWalkError(f"q has head dimension {dq}, the cache {d}")
+    if tables.dim() != 2 or tables.shape[0] != batch:
+        raise SketchWalkError(f"tables of shape {tuple(tables.shape)}, ({batch}, b_max) needed")
+    dev = q.device
+    if O is None:
+        O = torch.empty_like(q)
+    wsb = decode_attn_q8_workspace_bytes(batch, h_q, h_kv, d)
+    if workspace is None or workspace.numel() < wsb:
+        workspace = torch.empty((wsb,), dtype=torch.uint8, device=dev)
+    _same_device(dev, cache["k"], tables, pos, idx, cnt, O, workspace)
+    with _on(dev):
+        rc = load().sw_sparse_attn_decode_q8(
+            _dtype_code(q), _dev(q, "q"), *pages, batch, h_q, h_kv, d, n_pages,
+            _dev(tables, "tables", torch.int32), tables.shape[1], B, _vec(pos, batch, "pos"),
+            _mat(idx, (batch, kmax), "idx"), _vec(cnt, batch, "cnt"), kmax, float(scale),
+            _mat(O, (batch, h_q, d), "O", q.dtype), _dev(workspace, "workspace", torch.uint8),
+            workspace.numel(), _stream(dev))
+    _check(rc, "sw_sparse_attn_decode_q8")
+    return O
+
+
+def decode_step_q8(q_new: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, cache: dict,
+                   tables: torch.Tensor, slots: torch.Tensor, state: torch.Tensor, pos: torch.Tensor,
+                   signs: torch.Tensor, cols: torch.Tensor, s: int = 8, walk_variant: int = WALK_POWER,
+                   k: int = 0, density_pct: int = 20, flags: int = FORCE_BOTH, kmax: Optional[int] = None,
+                   scale: float = 0.0, out: Optional[dict] = None,
+                   workspace: Optional[torch.Tensor] = None) -> dict:
+    """decode_step over a paged 8-bit cache of stacked layers: the new tokens go to
+    ``slots`` [batch] (block_tables with rows=1), the attention reads through ``tables``
+    [batch][b_max]. Returns what decode_step returns."""
+    L, batch, h_q, d = q_new.shape
+    n_pages, h_kv, B, dc, pages = _pool(cache, L)
+    dev = q_new.device
+    if dc != d or tuple(k_new.shape) != (L, batch, h_kv, d) or v_new.shape != k_new.shape:
+        raise SketchWalkError(f"k_new, v_new of shape {tuple(k_new.shape)}, {tuple(v_new.shape)}: "
+                              f"({L}, {batch}, {h_kv}, {dc}) needed")
+    if tables.dim() != 2 or tables.shape[0] != batch:
+        raise SketchWalkError(f"tables of shape {tuple(tables.shape)}, ({batch}, b_max) needed")
+    b_max, r = tables.shape[1], int(cols.numel())
+    if kmax is None:
+        kmax = select_max_count_decode(b_max, k=k, density_pct=density_pct, flags=flags)
+    if state.numel() != L * decode_state_bytes(batch, d, r, b_max):
+        raise SketchWalkError(f"state of {state.numel()} bytes, {L} * {decode_state_bytes(batch, d, r, b_max)} needed")
+    o = dict(out or {})
+    _fill(o, {"rows": (L, batch, b_max)}, torch.float64, dev)
+    _fill(o, {"idx": (L, batch, kmax), "cnt": (L, batch)}, torch.int32, dev)
+    if "O" not in o:
+        o["O"] = torch.empty_like(q_new)
+    least = decode_attn_q8_workspace_bytes(batch, h_q, h_kv, d)
+    if workspace is None or workspace.numel() < least:
+        wsb = int(load().sw_decode_step_q8_workspace_bytes(batch, h_q, h_kv, d))
+        workspace = torch.empty((wsb,), dtype=torch.uint8, device=dev)
+    _same_device(dev, k_new, v_new, cache["k"], tables, slots, state, pos, signs, cols, workspace, *o.values())
+    with _on(dev):
+        rc = load().sw_decode_step_q8(
+            _dtype_code(q_new), L, batch, h_q, h_kv, d, r, n_pages, B, b_max, _dev(q_new, "q_new"),
+            _dev(k_new, "k_new", q_new.dtype), _dev(v_new, "v_new", q_new.dtype), *pages,
+            _dev(tables, "tables", torch.int32), _vec(slots, batch, "slots"),
+            _dev(state, "state", torch.uint8), _vec(pos, batch, "pos"), _mat(signs, (d,), "signs", torch.int8),
+            _dev(cols, "cols", torch.int32), s, walk_variant, k, density_pct, flags, kmax, float(scale),
+            _mat(o["rows"], (L, batch, b_max), "rows", torch.float64), _mat(o["idx"], (L, batch, kmax), "idx"),
+            _mat(o["cnt"], (L, batch), "cnt"), _mat(o["O"], (L, batch, h_q, d), "O", q_new.dtype),
+            _dev(workspace, "workspace", torch.uint8), workspace.numel(), _stream(dev))
+    _check(rc, "sw_decode_step_q8")
     return o

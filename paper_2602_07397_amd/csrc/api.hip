@@ -563,4 +563,244 @@ int sw_decode_step(int dtype, int layers, int batch, int h_q, int h_kv, int d, i
   return ok();
 }
 
+// ---------------------------------------------------------------------------
+// paged 8-bit cache
+// ---------------------------------------------------------------------------
+
+static int check_pool(int n_pages, int h_kv, int d, int B) {
+  if (h_kv < 1 || h_kv > 1024) return fail(SW_ERR_INVALID_ARG, "h_kv=%d outside [1, 1024]", h_kv);
+  if (d != 64 && d != 128) return fail(SW_ERR_UNSUPPORTED, "8-bit cache head dim d=%d (64 or 128)", d);
+  if (B < 16 || B > 1024 || B % 16 != 0)
+    return fail(SW_ERR_INVALID_ARG, "B=%d must be a multiple of 16 in [16, 1024]", B);
+  if (n_pages < 1 || (int64_t)n_pages * B >= (int64_t)1 << 31)
+    return fail(SW_ERR_INVALID_ARG, "n_pages=%d must be positive and n_pages * B below 2^31", n_pages);
+  return SW_OK;
+}
+
+static int check_pages(const void* k_pages, const void* v_pages, const uint8_t* k_scale,
+                       const uint8_t* v_scale) {
+  CHECK(check_ptr(k_pages, 16, "k_pages"));
+  CHECK(check_ptr(v_pages, 16, "v_pages"));
+  CHECK(check_ptr(k_scale, 1, "k_scale"));
+  CHECK(check_ptr(v_scale, 1, "v_scale"));
+  return SW_OK;
+}
+
+int sw_block_tables(int n_seqs, int B, int b_max, const int32_t* old_len, const int32_t* new_len,
+                    int32_t* tables, int32_t* free_pages, int32_t* n_free, int n_pages, int rows,
+                    int64_t n_slots, int32_t* slots, int32_t* cu_seqlens, int32_t* pos,
+                    int32_t* status, void* stream) {
+  if (n_seqs < 1 || n_seqs > 65536) return fail(SW_ERR_INVALID_ARG, "n_seqs=%d outside [1, 65536]", n_seqs);
+  CHECK(check_pool(n_pages, 1, 64, B));
+  if (b_max < 1 || (int64_t)b_max * B >= (int64_t)1 << 31)
+    return fail(SW_ERR_INVALID_ARG, "b_max=%d must be positive and b_max * B below 2^31", b_max);
+  if (rows < 0) return fail(SW_ERR_INVALID_ARG, "rows=%d < 0", rows);
+  if (n_slots < 0 || n_slots >= (int64_t)1 << 31)
+    return fail(SW_ERR_INVALID_ARG, "n_slots=%lld outside [0, 2^31)", (long long)n_slots);
+  if (rows > 0 && n_slots != (int64_t)n_seqs * rows)
+    return fail(SW_ERR_INVALID_ARG, "n_slots=%lld must be n_seqs * rows = %lld", (long long)n_slots,
+                (long long)n_seqs * rows);
+  CHECK(check_ptr(old_len, 4, "old_len"));
+  CHECK(check_ptr(new_len, 4, "new_len"));
+  CHECK(check_ptr(tables, 4, "tables"));
+  CHECK(check_ptr(free_pages, 4, "free_pages"));
+  CHECK(check_ptr(n_free, 4, "n_free"));
+  if (n_slots > 0) CHECK(check_ptr(slots, 4, "slots"));
+  CHECK(check_ptr(cu_seqlens, 4, "cu_seqlens"));
+  CHECK(check_ptr(pos, 4, "pos"));
+  CHECK(check_ptr(status, 4, "status"));
+  hipError_t e = sw::launch_block_tables(n_seqs, B, b_max, old_len, new_len, tables, free_pages, n_free,
+                                         n_pages, rows, (int)n_slots, slots, cu_seqlens, pos, status,
+                                         reinterpret_cast<hipStream_t>(stream));
+  return hip_status(e, "sw_block_tables launch");
+}
+
+int sw_kv_append_q8(int dtype, const void* k, const void* v, int64_t k_head_stride,
+                    int64_t k_token_stride, int64_t v_head_stride, int64_t v_token_stride, int64_t N,
+                    int n_seqs, const int32_t* cu_seqlens, const int32_t* slots, int n_pages,
+                    int h_kv, int d, int B, void* k_pages, void* v_pages, uint8_t* k_scale,
+                    uint8_t* v_scale, void* stream) {
+  if (dtype != SW_F32 && dtype != SW_BF16) return fail(SW_ERR_INVALID_ARG, "dtype=%d", dtype);
+  CHECK(check_pool(n_pages, h_kv, d, B));
+  if (N < 0 || N >= (int64_t)1 << 31) return fail(SW_ERR_INVALID_ARG, "N=%lld outside [0, 2^31)", (long long)N);
+  if (cu_seqlens && (n_seqs < 1 || n_seqs > 65536))
+    return fail(SW_ERR_INVALID_ARG, "n_seqs=%d outside [1, 65536]", n_seqs);
+  if (!cu_seqlens && N > SW_MAX_APPEND_TOKENS)
+    return fail(SW_ERR_UNSUPPORTED, "N=%lld tokens without cu_seqlens, at most %d", (long long)N,
+                SW_MAX_APPEND_TOKENS);
+  const int64_t strides[4] = {k_head_stride, k_token_stride, v_head_stride, v_token_stride};
+  const int piece = dtype == SW_BF16 ? 8 : 4;
+  for (int64_t x : strides)
+    if (x < 0 || x % piece != 0)
+      return fail(SW_ERR_INVALID_ARG, "stride %lld must be a multiple of %d elements", (long long)x, piece);
+  CHECK(check_pages(k_pages, v_pages, k_scale, v_scale));
+  if (N == 0) return ok();
+  CHECK(check_ptr(k, 16, "k"));
+  CHECK(check_ptr(v, 16, "v"));
+  CHECK(check_ptr(slots, 4, "slots"));
+  if (cu_seqlens && !aligned(cu_seqlens, 4)) return fail(SW_ERR_INVALID_ARG, "cu_seqlens misaligned");
+  const sw::TokenStrides sd{k_head_stride, k_token_stride, v_head_stride, v_token_stride, 0};
+  hipError_t e = sw::launch_kv_append_q8(dtype, 1, k, v, sd, (int)N, n_seqs, cu_seqlens, slots, n_pages,
+                                         h_kv, d, B, k_pages, v_pages, k_scale, v_scale,
+                                         reinterpret_cast<hipStream_t>(stream));
+  return hip_status(e, "sw_kv_append_q8 launch");
+}
+
+int sw_kv_fetch_q8(int dtype, const void* k_pages, const void* v_pages, const uint8_t* k_scale,
+                   const uint8_t* v_scale, int n_pages, int h_kv, int d, int B, int n_seqs, int b_max,
+                   const int32_t* tables, const int32_t* first, const int32_t* cu_seqlens, int64_t N,
+                   void* K, void* V, void* stream) {
+  if (dtype != SW_F32 && dtype != SW_BF16) return fail(SW_ERR_INVALID_ARG, "dtype=%d", dtype);
+  CHECK(check_pool(n_pages, h_kv, d, B));
+  if (n_seqs < 1 || n_seqs > 65536) return fail(SW_ERR_INVALID_ARG, "n_seqs=%d outside [1, 65536]", n_seqs);
+  if (b_max < 1 || (int64_t)b_max * B >= (int64_t)1 << 31)
+    return fail(SW_ERR_INVALID_ARG, "b_max=%d must be positive and b_max * B below 2^31", b_max);
+  if (N < 0 || N >= (int64_t)1 << 31) return fail(SW_ERR_INVALID_ARG, "N=%lld outside [0, 2^31)", (long long)N);
+  CHECK(check_pages(k_pages, v_pages, k_scale, v_scale));
+  CHECK(check_ptr(tables, 4, "tables"));
+  CHECK(check_ptr(cu_seqlens, 4, "cu_seqlens"));
+  if (first && !aligned(first, 4)) return fail(SW_ERR_INVALID_ARG, "first misaligned");
+  if (N == 0) return ok();
+  CHECK(check_ptr(K, 16, "K"));
+  CHECK(check_ptr(V, 16, "V"));
+  hipError_t e = sw::launch_kv_fetch_q8(dtype, k_pages, v_pages, k_scale, v_scale, n_pages, h_kv, d, B,
+                                        n_seqs, b_max, tables, first, cu_seqlens, (int)N, K, V,
+                                        reinterpret_cast<hipStream_t>(stream));
+  return hip_status(e, "sw_kv_fetch_q8 launch");
+}
+
+// Shapes of the decode attention over the 8-bit cache.
+static int check_attn_q8(int batch, int h_q, int h_kv) {
+  CHECK(check_heads(h_q, h_kv));
+  if (h_q / h_kv > 16)
+    return fail(SW_ERR_UNSUPPORTED, "8-bit decode attention needs h_q/h_kv in [1, 16], got %d", h_q / h_kv);
+  if (batch < 1 || batch > 65536) return fail(SW_ERR_INVALID_ARG, "batch=%d outside [1, 65536]", batch);
+  // a launch holds less than 2^32 threads
+  if ((int64_t)batch * h_q >= (int64_t)1 << 24)
+    return fail(SW_ERR_UNSUPPORTED, "batch * h_q = %lld, below 2^24 needed", (long long)batch * h_q);
+  return SW_OK;
+}
+
+int64_t sw_decode_attn_q8_workspace_bytes(int batch, int h_q, int h_kv, int d) {
+  if (check_attn_q8(batch, h_q, h_kv) != SW_OK) return -1;
+  if (d != 64 && d != 128) {
+    fail(SW_ERR_UNSUPPORTED, "8-bit cache head dim d=%d (64 or 128)", d);
+    return -1;
+  }
+  return sw_decode_attn_workspace_bytes(batch, h_q, h_kv, d);
+}
+
+int sw_sparse_attn_decode_q8(int dtype, const void* q, const void* k_pages, const void* v_pages,
+                             const uint8_t* k_scale, const uint8_t* v_scale, int batch, int h_q,
+                             int h_kv, int d, int n_pages, const int32_t* tables, int b_max, int B,
+                             const int32_t* pos, const int32_t* idx, const int32_t* cnt, int kmax,
+                             float scale, void* O, void* workspace, int64_t workspace_bytes,
+                             void* stream) {
+  if (dtype != SW_F32 && dtype != SW_BF16) return fail(SW_ERR_INVALID_ARG, "dtype=%d", dtype);
+  CHECK(check_attn_q8(batch, h_q, h_kv));
+  CHECK(check_pool(n_pages, h_kv, d, B));
+  if (b_max < 1 || (int64_t)b_max * B >= (int64_t)1 << 31)
+    return fail(SW_ERR_INVALID_ARG, "b_max=%d must be positive and b_max * B below 2^31", b_max);
+  if (kmax < 1) return fail(SW_ERR_INVALID_ARG, "kmax=%d < 1", kmax);
+  CHECK(check_pages(k_pages, v_pages, k_scale, v_scale));
+  CHECK(check_ptr(q, 16, "q"));
+  CHECK(check_ptr(O, 16, "O"));
+  CHECK(check_ptr(tables, 4, "tables"));
+  CHECK(check_ptr(pos, 4, "pos"));
+  CHECK(check_ptr(idx, 4, "idx"));
+  CHECK(check_ptr(cnt, 4, "cnt"));
+  const int64_t need = sw_decode_attn_q8_workspace_bytes(batch, h_q, h_kv, d);
+  CHECK(check_ptr(workspace, 256, "workspace"));
+  if (workspace_bytes < need)
+    return fail(SW_ERR_INVALID_ARG, "workspace_bytes=%lld < required %lld",
+                (long long)workspace_bytes, (long long)need);
+  if (!(scale > 0.0f)) scale = 1.0f / sqrtf((float)d);
+  hipError_t e = sw::launch_attn_decode_q8(dtype, 1, q, k_pages, v_pages, k_scale, v_scale, batch, h_q,
+                                           h_kv, d, n_pages, tables, b_max, B, pos, idx, cnt, kmax, scale,
+                                           O, reinterpret_cast<float*>(workspace),
+                                           reinterpret_cast<hipStream_t>(stream));
+  return hip_status(e, "sw_sparse_attn_decode_q8 launch");
+}
+
+// As sw_decode_step_workspace_bytes: eight layers in 64 MiB at most.
+int64_t sw_decode_step_q8_workspace_bytes(int batch, int h_q, int h_kv, int d) {
+  const int64_t one = sw_decode_attn_q8_workspace_bytes(batch, h_q, h_kv, d);
+  if (one < 0) return one;
+  int64_t n = ((int64_t)64 << 20) / one;
+  n = n < 1 ? 1 : n > 8 ? 8 : n;
+  return n * one;
+}
+
+int sw_decode_step_q8(int dtype, int layers, int batch, int h_q, int h_kv, int d, int r, int n_pages,
+                      int B, int b_max, const void* q_new, const void* k_new, const void* v_new,
+                      void* k_pages, void* v_pages, uint8_t* k_scale, uint8_t* v_scale,
+                      const int32_t* tables, const int32_t* slots, void* state, const int32_t* pos,
+                      const int8_t* signs, const int32_t* cols, int s, int walk_variant, int k,
+                      int density_pct, uint32_t flags, int kmax, float scale, double* rows,
+                      int32_t* idx, int32_t* cnt, void* O, void* workspace, int64_t workspace_bytes,
+                      void* stream) {
+  if (dtype != SW_F32 && dtype != SW_BF16) return fail(SW_ERR_INVALID_ARG, "dtype=%d", dtype);
+  if (layers < 1 || layers > 65535) return fail(SW_ERR_INVALID_ARG, "layers=%d outside [1, 65535]", layers);
+  if (walk_variant == SW_WALK_SOFTMAX || walk_variant == SW_WALK_MATPOW)
+    return fail(SW_ERR_UNSUPPORTED, "walk variant %d is not available in decode", walk_variant);
+  if (walk_variant != SW_WALK_POWER && walk_variant != SW_WALK_RELU)
+    return fail(SW_ERR_INVALID_ARG, "unknown walk variant %d", walk_variant);
+  if (s < 1 || s > 64) return fail(SW_ERR_INVALID_ARG, "s=%d outside [1, 64]", s);
+  CHECK(check_attn_q8(batch, h_q, h_kv));
+  if (batch > SW_MAX_APPEND_TOKENS)
+    return fail(SW_ERR_UNSUPPORTED, "batch=%d, at most %d", batch, SW_MAX_APPEND_TOKENS);
+  CHECK(check_pool(n_pages, h_kv, d, B));
+  CHECK(check_decode_shape(batch, d, r, b_max, B));
+  CHECK(check_budget_args(k, density_pct, flags));
+  const int need_k = last_row_budget(b_max, k, density_pct, flags);
+  if (kmax < need_k) return fail(SW_ERR_INVALID_ARG, "kmax=%d < largest budget %d", kmax, need_k);
+  CHECK(check_ptr(q_new, 16, "q_new"));
+  CHECK(check_ptr(k_new, 16, "k_new"));
+  CHECK(check_ptr(v_new, 16, "v_new"));
+  CHECK(check_pages(k_pages, v_pages, k_scale, v_scale));
+  CHECK(check_ptr(tables, 4, "tables"));
+  CHECK(check_ptr(slots, 4, "slots"));
+  CHECK(check_ptr(state, 256, "state"));
+  CHECK(check_ptr(pos, 4, "pos"));
+  CHECK(check_ptr(signs, 1, "signs"));
+  CHECK(check_ptr(cols, 4, "cols"));
+  CHECK(check_ptr(rows, 8, "rows"));
+  CHECK(check_ptr(idx, 4, "idx"));
+  CHECK(check_ptr(cnt, 4, "cnt"));
+  CHECK(check_ptr(O, 16, "O"));
+  const int64_t need = sw_decode_attn_q8_workspace_bytes(batch, h_q, h_kv, d);
+  CHECK(check_ptr(workspace, 256, "workspace"));
+  if (workspace_bytes < need)
+    return fail(SW_ERR_INVALID_ARG, "workspace_bytes=%lld < required %lld",
+                (long long)workspace_bytes, (long long)need);
+  if (!(scale > 0.0f)) scale = 1.0f / sqrtf((float)d);
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  const int64_t kv_step = (int64_t)batch * h_kv * d;
+  const sw::TokenStrides sd{d, (int64_t)h_kv * d, d, (int64_t)h_kv * d, kv_step};
+  hipError_t e = sw::launch_kv_append_q8(dtype, layers, k_new, v_new, sd, batch, 0, nullptr, slots,
+                                         n_pages, h_kv, d, B, k_pages, v_pages, k_scale, v_scale, st);
+  if (e != hipSuccess) return hip_status(e, "sw_decode_step_q8 launch");
+  e = sw::launch_decode_layers(dtype, layers, q_new, k_new, v_new, nullptr, nullptr, 0, batch, h_q, h_kv,
+                               d, B, pos, signs, cols, r, b_max, static_cast<char*>(state), s,
+                               walk_variant == SW_WALK_RELU, rows, k, density_pct, flags, idx, cnt, kmax,
+                               st);
+  if (e != hipSuccess) return hip_status(e, "sw_decode_step_q8 launch");
+  const size_t esz = dtype == SW_BF16 ? 2 : 4;
+  const int64_t q_step = (int64_t)batch * h_q * d * esz;
+  const int64_t pool = (int64_t)n_pages * h_kv, page_step = pool * B * d;
+  const int64_t per = workspace_bytes / need;    // layers whose partials share a launch
+  for (int64_t l = 0; l < layers; l += per) {
+    const int n = (int)(layers - l < per ? layers - l : per);
+    e = sw::launch_attn_decode_q8(dtype, n, static_cast<const char*>(q_new) + l * q_step,
+                                  static_cast<const char*>(k_pages) + l * page_step,
+                                  static_cast<const char*>(v_pages) + l * page_step, k_scale + l * pool,
+                                  v_scale + l * pool, batch, h_q, h_kv, d, n_pages, tables, b_max, B, pos,
+                                  idx + l * batch * kmax, cnt + l * batch, kmax, scale,
+                                  static_cast<char*>(O) + l * q_step, reinterpret_cast<float*>(workspace),
+                                  st);
+    if (e != hipSuccess) return hip_status(e, "sw_decode_step_q8 launch");
+  }
+  return ok();
+}
+
 }  // extern "C"

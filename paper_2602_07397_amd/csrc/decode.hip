@@ -363,7 +363,8 @@ struct LayerStrides {
 // The one-call step: steps 1-4 of every layer in one launch (blockIdx.z is
 // the layer). A launch per layer is latency: about 8 us each at batch 1,
 // where a layer has 9 workgroups; together the layers fill the chip.
-template <typename T>
+// APPEND: with the KV append (a contiguous cache).
+template <typename T, bool APPEND>
 __global__ __launch_bounds__(256) void decode_sketch_layers_kernel(
     const T* __restrict__ q_new, const T* __restrict__ k_new, int h_q, int h_kv, int d, int B,
     const int32_t* __restrict__ pos, const int8_t* __restrict__ signs,
@@ -376,9 +377,9 @@ __global__ __launch_bounds__(256) void decode_sketch_layers_kernel(
     using C = std::conditional_t<std::is_const_v<std::remove_pointer_t<decltype(p)>>, const char, char>;
     return reinterpret_cast<decltype(p)>(reinterpret_cast<C*>(p) + l * step);
   };
-  decode_sketch_body<T, true>(at(q_new, ls.q), at(k_new, ls.kv), h_q, h_kv, d, B, pos, signs, cols, r,
-                              batch, b_max, state + l * ls.state, at(v_new, ls.kv), at(Kc, ls.cache),
-                              at(Vc, ls.cache), T_max, blockIdx.x, blockIdx.y, lds);
+  decode_sketch_body<T, APPEND>(at(q_new, ls.q), at(k_new, ls.kv), h_q, h_kv, d, B, pos, signs, cols,
+                                r, batch, b_max, state + l * ls.state, at(v_new, ls.kv),
+                                at(Kc, ls.cache), at(Vc, ls.cache), T_max, blockIdx.x, blockIdx.y, lds);
 }
 
 // ---------------------------------------------------------------------------
@@ -1023,7 +1024,7 @@ hipError_t launch_decode_walk(const char* state, int batch, int d, int r, int b_
 
 namespace {
 
-template <typename T>
+template <typename T, bool APPEND>
 void launch_sketch_layers_t(int layers, const void* q_new, const void* k_new, const void* v_new,
                             void* Kc, void* Vc, int T_max, int batch, int h_q, int h_kv, int d, int B,
                             const int32_t* pos, const int8_t* signs, const int32_t* cols, int r,
@@ -1038,8 +1039,9 @@ void launch_sketch_layers_t(int layers, const void* q_new, const void* k_new, co
   for (int l0 = 0; l0 < layers; l0 += kMaxZ) {
     const int nz = layers - l0 < kMaxZ ? layers - l0 : kMaxZ;
     auto at = [l0](const void* p, long long step) { return static_cast<const char*>(p) + l0 * step; };
-    hipLaunchKernelGGL(decode_sketch_layers_kernel<T>, dim3((unsigned)batch, chunks, (unsigned)nz),
-                       dim3(256), 0, st, reinterpret_cast<const T*>(at(q_new, ls.q)),
+    hipLaunchKernelGGL((decode_sketch_layers_kernel<T, APPEND>),
+                       dim3((unsigned)batch, chunks, (unsigned)nz), dim3(256), 0, st,
+                       reinterpret_cast<const T*>(at(q_new, ls.q)),
                        reinterpret_cast<const T*>(at(k_new, ls.kv)), h_q, h_kv, d, B, pos, signs, cols,
                        r, batch, b_max, state + l0 * ls.state,
                        reinterpret_cast<const T*>(at(v_new, ls.kv)),
@@ -1068,12 +1070,15 @@ hipError_t launch_decode_layers(int dtype, int layers, const void* q_new, const 
                                 const int32_t* cols, int r, int b_max, char* state, int s_exp,
                                 bool relu, double* rows, int k, int pct, uint32_t flags, int32_t* idx,
                                 int32_t* cnt, int kmax, hipStream_t st) {
-  if (dtype == SW_BF16)
-    launch_sketch_layers_t<uint16_t>(layers, q_new, k_new, v_new, Kc, Vc, T_max, batch, h_q, h_kv, d, B,
-                                     pos, signs, cols, r, b_max, state, st);
-  else
-    launch_sketch_layers_t<float>(layers, q_new, k_new, v_new, Kc, Vc, T_max, batch, h_q, h_kv, d, B,
-                                  pos, signs, cols, r, b_max, state, st);
+#define SW_SKETCH_LAYERS(T, APPEND)                                                                \
+  launch_sketch_layers_t<T, APPEND>(layers, q_new, k_new, v_new, Kc, Vc, T_max, batch, h_q, h_kv, d, \
+                                    B, pos, signs, cols, r, b_max, state, st)
+  if (dtype == SW_BF16) {
+    if (Kc) SW_SKETCH_LAYERS(uint16_t, true); else SW_SKETCH_LAYERS(uint16_t, false);
+  } else {
+    if (Kc) SW_SKETCH_LAYERS(float, true); else SW_SKETCH_LAYERS(float, false);
+  }
+#undef SW_SKETCH_LAYERS
   const DecodeLayout L = decode_layout(batch, d, r, b_max);
   const long long row_step = (long long)batch * b_max;
   const int pairs = strip_pairs(batch, d, r, b_max);

@@ -109,6 +109,7 @@ hipError_t launch_decode_walk(const char* state, int batch, int d, int r, int b_
 // sketch with the KV append of all layers in one launch, then one launch per
 // layer for the walk row with the selection of the layer before it, and a
 // last one for the last layer's selection. Buffers are stacked over layers.
+// Kc NULL: no append.
 hipError_t launch_decode_layers(int dtype, int layers, const void* q_new, const void* k_new,
                                 const void* v_new, void* Kc, void* Vc, int T_max, int batch, int h_q,
                                 int h_kv, int d, int B, const int32_t* pos, const int8_t* signs,
@@ -132,5 +133,48 @@ hipError_t launch_attn_decode(int dtype, int layers, const void* q, const void* 
                               int batch, int h_q, int h_kv, int d, int T_max, int B,
                               const int32_t* pos, const int32_t* idx, const int32_t* cnt, int kmax,
                               float scale, void* O, float* ws, hipStream_t st);
+
+// The merge of the 8-bit cache's split-K partials of `layers` layers
+// (attn_decode.hip), maxima in log2 units.
+hipError_t launch_attn_merge_q8(int dtype, int layers, int batch, int h_q, int d, int S,
+                                const float* ws, void* O, hipStream_t st);
+
+// ---------------------------------------------------------------------------
+// paged 8-bit cache
+// ---------------------------------------------------------------------------
+
+// Strides of the new tokens' keys and values in elements: from one head to the
+// next, one token to the next, and one layer to the next of stacked buffers.
+struct TokenStrides {
+  long long k_head, k_tok, v_head, v_tok, layer;
+};
+
+// Elements from one layer to the next (pool: pages times heads).
+struct DecodeQ8Steps {
+  long long q, pool, idx, cnt, ws;
+};
+
+hipError_t launch_block_tables(int n_seqs, int B, int b_max, const int32_t* old_len,
+                               const int32_t* new_len, int32_t* tables, int32_t* free_pages,
+                               int32_t* n_free, int n_pages, int rows, int n_slots, int32_t* slots,
+                               int32_t* cu, int32_t* pos, int32_t* status, hipStream_t st);
+
+// cu NULL: every token by its slot alone.
+hipError_t launch_kv_append_q8(int dtype, int layers, const void* k, const void* v,
+                               const TokenStrides& sd, int N, int n_seqs, const int32_t* cu,
+                               const int32_t* slots, int n_pages, int h_kv, int d, int B, void* Kp,
+                               void* Vp, uint8_t* ks, uint8_t* vs, hipStream_t st);
+
+hipError_t launch_kv_fetch_q8(int dtype, const void* Kp, const void* Vp, const uint8_t* ks,
+                              const uint8_t* vs, int n_pages, int h_kv, int d, int B, int n_seqs,
+                              int b_max, const int32_t* tables, const int32_t* first, const int32_t* cu,
+                              int N, void* K, void* V, hipStream_t st);
+
+// ws: decode_attn_splits(batch, h_kv) partials per (sequence, query head) and layer.
+hipError_t launch_attn_decode_q8(int dtype, int layers, const void* q, const void* Kp, const void* Vp,
+                                 const uint8_t* ks, const uint8_t* vs, int batch, int h_q, int h_kv,
+                                 int d, int n_pages, const int32_t* tables, int b_max, int B,
+                                 const int32_t* pos, const int32_t* idx, const int32_t* cnt, int kmax,
+                                 float scale, void* O, float* ws, hipStream_t st);
 
 }  // namespace sw

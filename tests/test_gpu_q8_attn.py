@@ -1,0 +1,392 @@
+"""Decode attention over the paged 8-bit cache, and the one-call step over it."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import _q8_ref as R
+import oracle as O
+import synth
+from paper_2602_07397_amd import binding as sw
+
+pytestmark = pytest.mark.gpu
+
+U = pytest.importorskip("_gpu_util")
+
+
+def _i32(x):
+    return torch.tensor(x, dtype=torch.int32, device=U.DEV)
+
+
+def _cache(seed, P, h, B, d, big=1.0):
+    """Random codes, scales that differ from page to page; unused places hold any byte,
+    NaN codes among them (the test that calls for it overwrites the used ones)."""
+    g = torch.Generator(device=U.DEV).manual_seed(seed)
+    cache = sw.new_cache_q8(P, h, B, d, U.DEV)
+    for n in "kv":
+        x = torch.randn(cache[n].shape, generator=g, device=U.DEV) * 64
+        cache[n].copy_(x.clamp_(-448, 448).to(torch.float8_e4m3fn))
+        e = torch.randint(-1, 2, (P, h), generator=g, device=U.DEV) - 6 + (int(math.log2(big)) if n == "k" else 0)
+        cache[n + "_scale"].copy_((e + 127).to(torch.uint8))
+    return cache
+
+
+def _case(seed, batch, h_q, h_kv, d, B, ctx, dtype, density=0.3, big=1.0):
+    rng = np.random.default_rng(seed)
+    pos = [int(rng.integers(0, ctx)) for _ in range(batch)]
+    pos[0] = ctx - 1
+    b_max = -(-ctx // B)
+    P = batch * b_max + 3
+    tables = rng.permutation(P)[:batch * b_max].reshape(batch, b_max).astype(np.int32)
+    sels = [sorted({0, p // B} | {j for j in range(p // B) if rng.uniform() < density}) if p >= 0 else [0]
+            for p in pos]
+    kmax = max(len(s) for s in sels) + 1
+    idx = np.full((batch, kmax), -1, dtype=np.int32)
+    for b, s in enumerate(sels):
+        idx[b, :len(s)] = s
+    q = torch.from_numpy(rng.normal(size=(batch, h_q, d))).to(dtype)
+    return dict(q=q, cache=_cache(seed, P, h_kv, B, d, big), tables=tables, pos=pos, idx=idx,
+                cnt=np.array([len(s) for s in sels], dtype=np.int32), kmax=kmax, B=B, P=P)
+
+
+def _run(c, **kw):
+    return sw.sparse_attn_decode_q8(U.to_dev(c["q"]), c["cache"], U.to_dev(c["tables"]), _i32(c["pos"]),
+                                    U.to_dev(c["idx"]), U.to_dev(c["cnt"]), c["kmax"], **kw)
+
+
+def _selected(c, b):
+    """Pages and places of the tokens that count for sequence b, in list order."""
+    p, B = c["pos"][b], c["B"]
+    b_max = c["tables"].shape[1]
+    if p < 0 or p // B >= b_max:
+        return [], []
+    pages, places = [], []
+    for j in c["idx"][b, :max(0, min(int(c["cnt"][b]), c["kmax"]))]:
+        if j < 0 or j > p // B or not 0 <= c["tables"][b, j] < c["P"]:
+            continue
+        for o in range(min(B, p + 1 - j * B)):
+            pages.append(int(c["tables"][b, j]))
+            places.append(o)
+    return pages, places
+
+
+def _check(c, got, scale=None):
+    x, _ = R.cache_values(c["cache"])
+    d = c["q"].shape[2]
+    scale = scale or 1.0 / math.sqrt(d)
+    got = got.double().cpu().numpy()
+    for b in range(len(c["pos"])):
+        pages, places = _selected(c, b)
+        if not pages:
+            assert np.all(got[b] == 0.0), b
+            continue
+        K = x["k"][pages, :, places].transpose(1, 0, 2)
+        V = x["v"][pages, :, places].transpose(1, 0, 2)
+        o, a, top = R.attention(c["q"][b].double().numpy(), K, V, scale)
+        err = np.abs(got[b] - o)
+        bound = R.attention_bound(c["q"].dtype, o, a, top, d, len(pages))
+        assert np.all(err <= bound), (b, float((err / bound).max()), float(err.max()))
+
+
+DT = [torch.bfloat16, torch.float32]
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("batch,h_q,h_kv,d,B,ctx", [
+    (1, 1, 1, 64, 16, 1), (1, 4, 4, 128, 64, 5000), (3, 8, 2, 128, 64, 700), (2, 28, 4, 128, 128, 1500),
+    (4, 16, 1, 64, 16, 333), (2, 6, 2, 64, 48, 1000), (5, 12, 4, 128, 80, 777), (1, 32, 8, 128, 1024, 9000),
+    (70, 8, 8, 64, 32, 200), (2, 10, 2, 128, 64, 64), (3, 18, 2, 64, 16, 17)])
+def test_attention(dtype, batch, h_q, h_kv, d, B, ctx):
+    c = _case(batch * 1000 + ctx, batch, h_q, h_kv, d, B, ctx, dtype)
+    got = _run(c)
+    _check(c, got)
+    assert torch.equal(got, _run(c))                 # same inputs, same bits
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("ctx", [1, 15, 16, 17, 63, 64, 65, 127, 128, 129, 255, 257])
+def test_attention_at_group_edges(dtype, ctx):
+    c = _case(ctx, 2, 8, 2, 128, 64, ctx, dtype, density=1.0)
+    _check(c, _run(c))
+    c = _case(ctx + 7, 2, 4, 1, 64, 16, ctx, dtype, density=0.5)
+    _check(c, _run(c))
+
+
+@pytest.mark.parametrize("dtype", DT)
+def test_unused_places_may_hold_anything(dtype):
+    """Behind a sequence's end, in unlisted pages: NaN codes and the largest values."""
+    c = _case(21, 3, 8, 2, 64, 64, 400, dtype)
+    clean = _run(c)
+    used = {}
+    for b in range(3):
+        for pg, o in zip(*_selected(c, b)):
+            used.setdefault(pg, set()).add(o)
+    k, v = c["cache"]["k"].view(torch.uint8), c["cache"]["v"].view(torch.uint8)
+    for pg in range(c["P"]):
+        rest = [o for o in range(64) if o not in used.get(pg, ())]
+        if rest:
+            k[pg, :, rest] = 0x7f
+            v[pg, :, :, rest] = 0xff
+    assert torch.equal(clean, _run(c))
+
+
+@pytest.mark.parametrize("dtype", DT)
+def test_rows_without_a_token_and_pages_that_are_none(dtype):
+    c = _case(22, 7, 8, 4, 128, 32, 500, dtype)
+    c["pos"][1] = -1                                 # idle
+    c["pos"][2] = 32 * c["tables"].shape[1]          # behind the table
+    c["cnt"][3] = 0                                  # nothing selected
+    c["tables"][4] = -1                              # no page at all
+    c["tables"][5, :] = c["P"] + np.arange(c["tables"].shape[1])
+    c["cnt"][6] = -5
+    c["cnt"][0] = c["kmax"] + 100                    # clamped
+    c["idx"][0, 1] = -7                              # entries to skip
+    c["idx"][0, 2] = 1 << 30
+    c["tables"][0, 0] = -2
+    _check(c, _run(c))
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("big", [16.0, 256.0])
+def test_large_logits(dtype, big):
+    c = _case(23, 2, 8, 2, 128, 64, 600, dtype, big=big)
+    got = _run(c)
+    assert torch.isfinite(got.float()).all()
+    _check(c, got)
+    _check(c, _run(c, scale=0.003), scale=0.003)
+
+
+def test_nan_of_a_token_that_counts_shows():
+    c = _case(24, 2, 4, 2, 64, 16, 100, torch.float32)
+    pg = int(c["tables"][0, 0])
+    c["cache"]["k"].view(torch.uint8)[pg, 1, 3, 5] = 0x7f
+    got = _run(c)
+    assert torch.isnan(got[0, 2:]).all() and torch.isfinite(got[0, :2]).all() and torch.isfinite(got[1]).all()
+
+
+@pytest.mark.parametrize("dtype", DT)
+def test_long_lists(dtype):
+    """More chunks than are listed at a time, blocks in any order and one of them twice."""
+    c = _case(25, 1, 8, 1, 64, 16, 16 * 33000, dtype, density=1.0)
+    n = int(c["cnt"][0])
+    c["idx"][0, :n] = c["idx"][0, :n][np.random.default_rng(1).permutation(n)]
+    _check(c, _run(c))
+    c = _case(26, 1, 4, 2, 128, 64, 1000, dtype)
+    n = int(c["cnt"][0])
+    c["idx"][0, n] = c["idx"][0, 0]
+    c["cnt"][0] = n + 1
+    _check(c, _run(c))
+
+
+def test_pool_behind_4_gib():
+    """Pages whose offset passes 32 bits."""
+    h, B, d = 8, 64, 128
+    P = (1 << 32) // (h * B * d) + 40
+    cache = {"k": torch.empty((P, h, B, d), dtype=torch.float8_e4m3fn, device=U.DEV),
+             "v": torch.empty((P, h, d, B), dtype=torch.float8_e4m3fn, device=U.DEV),
+             "k_scale": torch.full((P, h), 121, dtype=torch.uint8, device=U.DEV),
+             "v_scale": torch.full((P, h), 121, dtype=torch.uint8, device=U.DEV)}
+    tail = slice(P - 20, P)
+    for n in "kv":
+        cache[n][tail].copy_((torch.randn(cache[n][tail].shape, device=U.DEV) * 60).clamp(-448, 448).to(torch.float8_e4m3fn))
+    tables = np.arange(P - 1, P - 17, -1).astype(np.int32).reshape(2, 8)
+    small = {n: t[tail].contiguous() for n, t in cache.items()}
+    rng = np.random.default_rng(2)
+    q = U.to_dev(torch.from_numpy(rng.normal(size=(2, 32, d))).to(torch.bfloat16))
+    args = (_i32([511, 400]), _i32([[0, 2, 5, 7], [0, 1, 3, 6]]), _i32([4, 4]), 4)
+    new = torch.randn((2, h, d), device=U.DEV, dtype=torch.bfloat16).transpose(0, 1)
+    outs = []
+    for c, base in ((cache, 0), (small, P - 20)):
+        t = U.to_dev(tables - base)
+        slots = _i32([int((tables[0, 7] - base) * B + 63), int((tables[1, 6] - base) * B + 16)])
+        sw.kv_append_q8(new, new, slots, c)
+        K, V = sw.kv_fetch_q8(c, t, _i32([440, 380]), _i32([0, 72, 93]), 93)
+        outs.append((sw.sparse_attn_decode_q8(q, c, t, *args), K, V))
+    for a, b in zip(*outs):
+        assert torch.equal(a, b)
+
+
+def test_attention_in_two_streams_and_captured():
+    c1, c2 = (_case(s, 4, 32, 8, 128, 64, 3000, torch.bfloat16) for s in (31, 32))
+    want = [_run(c1), _run(c2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = []
+    for c, s in zip((c1, c2), streams):
+        with torch.cuda.stream(s):
+            got.append([_run(c) for _ in range(3)])
+    torch.cuda.synchronize()
+    for w, many in zip(want, got):
+        assert all(torch.equal(w, g) for g in many)
+    dev = {n: U.to_dev(c1[n]) for n in ("q", "tables", "idx", "cnt")}
+    pos = _i32(c1["pos"])
+    out = torch.empty_like(dev["q"])
+    ws = torch.empty((sw.decode_attn_q8_workspace_bytes(4, 32, 8, 128),), dtype=torch.uint8, device=U.DEV)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        sw.sparse_attn_decode_q8(dev["q"], c1["cache"], dev["tables"], pos, dev["idx"], dev["cnt"], c1["kmax"],
+                                 O=out, workspace=ws)
+    for i in range(4):
+        out.zero_()
+        g.replay()
+        assert torch.equal(out, want[0])
+        dev["q"].mul_(1.0)                           # the program's own work in between
+        torch.cuda.synchronize()
+
+
+# --------------------------------------------------------------------------- one-call step
+
+
+def _step_setup(dtype, h_q, h_kv, d, B, L, prompts, steps, seed):
+    w = synth.Workload("q8_step", 70 + seed, layers=L, h_q=h_q, h_kv=h_kv, d=d, B=B,
+                       dtype="bf16" if dtype == torch.bfloat16 else "f32", pct=30, needles=1,
+                       batch=len(prompts), kv_len=max(prompts), steps=steps)
+    signs, cols = synth.srht_params(w.d, w.r, w.seed)
+    ts, tc = U.to_dev(signs), U.to_dev(cols)
+    n = len(prompts)
+    b_max = -(-(max(prompts) + steps) // B)
+    P = sum(-(-(p + steps) // B) for p in prompts) + 2
+    pool = dict(tables=torch.full((n, b_max), -1, dtype=torch.int32, device=U.DEV),
+                free=torch.arange(P, dtype=torch.int32, device=U.DEV), n_free=_i32([P]))
+    cache = sw.new_cache_q8(P, h_kv, B, d, U.DEV, layers=L)
+    state = torch.zeros((L, sw.decode_state_bytes(n, d, w.r, b_max)), dtype=torch.uint8, device=U.DEV)
+    N = sum(prompts)
+    out = sw.block_tables(_i32([0] * n), _i32(prompts), B, pool["tables"], pool["free"], pool["n_free"], N)
+    assert int(out["status"]) == 0
+    for l in range(L):
+        layer = {k: t[l] for k, t in cache.items()}
+        Ks, Vs = [], []
+        for s, p in enumerate(prompts):
+            Q, K, V = (U.to_dev(x) for x in synth.decode_prefix_inputs(w, l, s, kv_len=p))
+            sk = sw.sketch_scores(Q, K, [0, p], B, ts, tc, want_means=True)
+            sw.decode_state_init(state[l], n, d, w.r, b_max, s, p, B, sk)
+            Ks.append(K)
+            Vs.append(V)
+        sw.kv_append_q8(torch.cat(Ks, 1), torch.cat(Vs, 1), out["slots"], layer, cu=out["cu"])
+    return w, ts, tc, pool, cache, state, b_max
+
+
+@pytest.mark.parametrize("dtype,h_q,h_kv,d,B,per_ws", [
+    (torch.bfloat16, 8, 2, 128, 64, None), (torch.float32, 4, 4, 64, 16, 1), (torch.bfloat16, 14, 2, 64, 32, 2)])
+def test_step_is_the_per_layer_calls(dtype, h_q, h_kv, d, B, per_ws):
+    """Steps across block borders, pages taken as they come, one sequence idle for a
+    step: bit for bit the per-layer calls, and the attention against 64 bits."""
+    L, prompts, steps = 3, [2 * B - 2, 1, 3 * B + 5], 5
+    w, ts, tc, pool, cache, state, b_max = _step_setup(dtype, h_q, h_kv, d, B, L, prompts, steps, h_q)
+    cache2 = {k: t.clone() for k, t in cache.items()}
+    state2 = state.clone()
+    n, lens = len(prompts), list(prompts)
+    kmax = sw.select_max_count_decode(b_max, density_pct=30)
+    ws = None
+    if per_ws:
+        ws = torch.empty((per_ws * sw.decode_attn_q8_workspace_bytes(n, h_q, h_kv, d),), dtype=torch.uint8, device=U.DEV)
+    for t in range(steps):
+        new = [x + 1 for x in lens]
+        if t == 2:
+            new[1] = lens[1]
+        tok = [synth.decode_step_inputs(w, t, l, batch=n) for l in range(L)]
+        q, k, v = (torch.stack([x[i] for x in tok]).to(U.DEV) for i in range(3))
+        bt = sw.block_tables(_i32(lens), _i32(new), B, pool["tables"], pool["free"], pool["n_free"], n, rows=1)
+        pos = torch.where(bt["slots"] < 0, -1, bt["pos"])           # an idle sequence is skipped
+        out = sw.decode_step_q8(q, k, v, cache, pool["tables"], bt["slots"], state, pos, ts, tc, density_pct=30,
+                                workspace=ws)
+        row = None
+        for l in range(L):
+            layer = {m: x[l] for m, x in cache2.items()}
+            sw.kv_append_q8(k[l].transpose(0, 1), v[l].transpose(0, 1), bt["slots"], layer)
+            sw.sketch_scores_decode(q[l], k[l], B, pos, ts, tc, b_max, state2[l])
+            row = sw.walk_update_decode(state2[l], n, d, w.r, b_max, B, pos, 8, row)
+            idx, cnt, _ = sw.select_topk_blocks_decode(row, B, pos, density_pct=30, kmax=kmax)
+            o = sw.sparse_attn_decode_q8(q[l], layer, pool["tables"], pos, idx, cnt, kmax)
+            on = [s for s in range(n) if pos[s] >= 0]
+            assert torch.equal(out["rows"][l][on], row[on]) and torch.equal(out["cnt"][l][on], cnt[on])
+            assert torch.equal(out["idx"][l][on], idx[on]) and torch.equal(out["O"][l], o)
+            c = dict(q=q[l].cpu(), cache=layer, tables=pool["tables"].cpu().numpy(), pos=pos.tolist(),
+                     idx=idx.cpu().numpy(), cnt=cnt.cpu().numpy(), kmax=kmax, B=B, P=cache["k"].shape[1])
+            _check(c, o)
+        for m in cache:
+            assert torch.equal(cache[m].view(torch.uint8), cache2[m].view(torch.uint8)), m
+        assert torch.equal(state, state2)
+        lens = new
+
+
+def test_step_follows_the_step_over_a_contiguous_cache():
+    """The same tokens through sw_decode_step (exact cache) and the 8-bit one: the sketch,
+    walk and selection are the same bits, the attention is that of the stored values."""
+    L, B, d, h_q, h_kv, prompts, steps = 2, 64, 128, 8, 2, [200, 130], 3
+    w, ts, tc, pool, cache, state, b_max = _step_setup(torch.bfloat16, h_q, h_kv, d, B, L, prompts, steps, 3)
+    n, T = 2, b_max * B
+    Kc = torch.zeros((L, n, h_kv, T, d), dtype=torch.bfloat16, device=U.DEV)
+    Vc = torch.zeros_like(Kc)
+    state2, lens = state.clone(), list(prompts)
+    for t in range(steps):
+        new = [x + 1 for x in lens]
+        tok = [synth.decode_step_inputs(w, t, l, batch=n) for l in range(L)]
+        q, k, v = (torch.stack([x[i] for x in tok]).to(U.DEV) for i in range(3))
+        bt = sw.block_tables(_i32(lens), _i32(new), B, pool["tables"], pool["free"], pool["n_free"], n, rows=1)
+        out = sw.decode_step_q8(q, k, v, cache, pool["tables"], bt["slots"], state, bt["pos"], ts, tc, density_pct=30)
+        # the contiguous cache holds the stored values, the new token's among them
+        for l in range(L):
+            layer = {m: x[l] for m, x in cache.items()}
+            for s in range(n):
+                K, V = sw.kv_fetch_q8(layer, pool["tables"][s:s + 1], None, _i32([0, new[s]]), new[s])
+                Kc[l, s, :, :new[s]], Vc[l, s, :, :new[s]] = K, V
+        ref = sw.decode_step(q, k, v, Kc.clone(), Vc.clone(), state2, bt["pos"], ts, tc, B, b_max, density_pct=30)
+        for m in ("rows", "idx", "cnt"):
+            assert torch.equal(out[m], ref[m]), m
+        assert torch.equal(state, state2)
+        for l in range(L):
+            got = sw.sparse_attn_decode(q[l], Kc[l], Vc[l], B, bt["pos"], out["idx"][l], out["cnt"][l], out["idx"].shape[2])
+            a = out["O"][l].float().abs().max()
+            # both round weights and outputs to bf16: each within 2^-8 of the weighted mean of |v|, and of itself
+            assert (out["O"][l].float() - got.float()).abs().max() <= 4 * 2.0 ** -8 * max(float(Vc.float().abs().max()), float(a))
+        lens = new
+
+
+def test_step_captured_replays():
+    L, B, d, h_q, h_kv, prompts = 2, 32, 64, 4, 2, [100, 31]
+    w, ts, tc, pool, cache, state, b_max = _step_setup(torch.bfloat16, h_q, h_kv, d, B, L, prompts, 8, 5)
+    n = 2
+    tok = [synth.decode_step_inputs(w, 0, l, batch=n) for l in range(L)]
+    q, k, v = (torch.stack([x[i] for x in tok]).to(U.DEV) for i in range(3))
+    old, new = _i32(prompts), _i32([x + 1 for x in prompts])
+    kmax = sw.select_max_count_decode(b_max, density_pct=30)
+    out = {"rows": torch.zeros((L, n, b_max), dtype=torch.float64, device=U.DEV),
+           "idx": torch.zeros((L, n, kmax), dtype=torch.int32, device=U.DEV),
+           "cnt": torch.zeros((L, n), dtype=torch.int32, device=U.DEV), "O": torch.zeros_like(q)}
+    bt = {"slots": _i32([0, 0]), "cu": _i32([0] * 3), "pos": _i32([0, 0]), "status": _i32([0])}
+    ws = torch.empty((sw.load().sw_decode_step_q8_workspace_bytes(n, h_q, h_kv, d),), dtype=torch.uint8, device=U.DEV)
+
+    def step():
+        sw.block_tables(old, new, B, pool["tables"], pool["free"], pool["n_free"], n, rows=1, out=bt)
+        sw.decode_step_q8(q, k, v, cache, pool["tables"], bt["slots"], state, bt["pos"], ts, tc, density_pct=30,
+                          kmax=kmax, out=out, workspace=ws)
+
+    saved = [t.clone() for t in (state, *pool.values(), *(x.view(torch.uint8) for x in cache.values()))]
+
+    def reset():
+        for t, s in zip((state, *pool.values(), *(x.view(torch.uint8) for x in cache.values())), saved):
+            t.copy_(s)
+        old.copy_(_i32(prompts))
+        new.copy_(_i32([x + 1 for x in prompts]))
+
+    wants = []
+    for _ in range(4):                               # eager: four tokens
+        step()
+        wants.append({m: x.clone() for m, x in out.items()})
+        old.add_(1)
+        new.add_(1)
+    reset()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    reset()
+    for want in wants:
+        g.replay()
+        for m in out:
+            assert torch.equal(out[m], want[m]), m
+        old.add_(1)
+        new.add_(1)
+        torch.cuda.synchronize()
