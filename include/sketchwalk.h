@@ -439,12 +439,14 @@ int sw_decode_step(int dtype, int layers, int batch, int h_q, int h_kv, int d, i
  *     [0, b_max * B], more new tokens than slots or than rows, or more pages
  *     given back than the pool has. With 1 and 2 nothing changes, cu_seqlens is
  *     0, every slot -1 and pos old_len - 1.
- * The buffers must not overlap.
+ * workspace: sw_block_tables_workspace_bytes(...) bytes, 8-byte aligned (may be
+ * NULL when that is 0); its contents are scratch. The buffers must not overlap.
  */
+int64_t sw_block_tables_workspace_bytes(int n_seqs, int64_t n_slots);
 int sw_block_tables(int n_seqs, int B, int b_max, const int32_t* old_len, const int32_t* new_len,
                     int32_t* tables, int32_t* free_pages, int32_t* n_free, int n_pages, int rows,
                     int64_t n_slots, int32_t* slots, int32_t* cu_seqlens, int32_t* pos,
-                    int32_t* status, void* stream);
+                    int32_t* status, void* workspace, int64_t workspace_bytes, void* stream);
 
 /*
  * sw_kv_append_q8 - writes N tokens' keys and values into the pages that their

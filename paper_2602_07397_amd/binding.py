@@ -8,7 +8,6 @@ built or cannot be loaded, every call raises.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 from typing import Optional, Sequence, Tuple
@@ -80,8 +79,9 @@ _SIGNATURES = {
     "sw_sparse_attn_decode_noalloc": (_c_int, [_c_int, _vp, _vp, _vp, _c_int, _c_int, _c_int, _c_int,
                                                _c_int, _c_int, _vp, _vp, _vp, _c_int, ctypes.c_float,
                                                _vp, _vp]),
+    "sw_block_tables_workspace_bytes": (_c_i64, [_c_int, _c_i64]),
     "sw_block_tables": (_c_int, [_c_int, _c_int, _c_int, _vp, _vp, _vp, _vp, _vp, _c_int, _c_int,
-                                 _c_i64, _vp, _vp, _vp, _vp, _vp]),
+                                 _c_i64, _vp, _vp, _vp, _vp, _vp, _c_i64, _vp]),
     "sw_kv_append_q8": (_c_int, [_c_int, _vp, _vp, _c_i64, _c_i64, _c_i64, _c_i64, _c_i64, _c_int, _vp,
                                  _vp, _c_int, _c_int, _c_int, _c_int, _vp, _vp, _vp, _vp, _vp]),
     "sw_kv_fetch_q8": (_c_int, [_c_int, _vp, _vp, _vp, _vp, _c_int, _c_int, _c_int, _c_int, _c_int,
@@ -555,75 +555,98 @@ def new_cache_q8(n_pages: int, h_kv: int, B: int, d: int, device, layers: Option
             "k_scale": zeros((n_pages, h_kv), torch.uint8), "v_scale": zeros((n_pages, h_kv), torch.uint8)}
 
 
-def _same_device(dev: torch.device, *tensors: Optional[torch.Tensor]) -> None:
-    for t in tensors:
-        if t is not None and t.device != dev:
-            raise SketchWalkError(f"all tensors must be on {dev}, got {t.device}")
+_I32 = torch.int32
+_U8 = torch.uint8
 
 
-_HERE_ALREADY = contextlib.nullcontext()
+def _at(t: torch.Tensor, dtype: torch.dtype, di: int, name: str) -> int:
+    """Address of a contiguous tensor of ``dtype`` on device ``di``. The calls of a decode
+    step take as long on the host as on the GPU: one test where all is well."""
+    if t.dtype is dtype and t.get_device() == di and t.is_contiguous():
+        return t.data_ptr()
+    _dev(t, name, dtype)
+    raise SketchWalkError(f"{name} is on {t.device}, not on cuda:{di} as the other tensors")
 
 
-def _on(dev: torch.device):
-    """Makes ``dev`` the current device where it is not (the launch goes to the current one)."""
-    if dev.type != "cuda":
-        raise SketchWalkError(f"tensors must be on a CUDA (HIP) device, got {dev}")
-    return _HERE_ALREADY if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
+def _vec(t: torch.Tensor, n: int, di: int, name: str) -> int:
+    """Address of a device int32 vector of n entries."""
+    if t.numel() != n:
+        raise SketchWalkError(f"{name} has {t.numel()} entries, {n} needed")
+    return _at(t, _I32, di, name)
+
+
+def _shaped(t: torch.Tensor, shape: tuple, name: str) -> None:
+    if t.shape != shape:
+        raise SketchWalkError(f"{name} of shape {tuple(t.shape)}, {shape} needed")
+
+
+def _gpu(t: torch.Tensor, name: str) -> int:
+    """Index of the GPU that ``t`` is on."""
+    di = t.get_device()
+    if di < 0:
+        raise SketchWalkError(f"{name} must be a CUDA (HIP) tensor")
+    return di
+
+
+def _launch(di: int, fn, *args) -> None:
+    """Calls ``fn`` on device ``di``'s current stream, on that device whichever is current."""
+    if torch._C._cuda_getDevice() == di:
+        rc = fn(*args, torch._C._cuda_getCurrentRawStream(di))
+    else:
+        with torch.cuda.device(di):
+            rc = fn(*args, torch._C._cuda_getCurrentRawStream(di))
+    if rc != SW_OK:
+        _check(rc, fn.__name__)
 
 
 def _pool(cache: dict, layers: Optional[int] = None):
-    """(n_pages, h_kv, B, d, pointers) of a cache as new_cache_q8 makes it."""
+    """(device index, n_pages, h_kv, B, d, pointers) of a cache as new_cache_q8 makes it."""
     k, v, ks, vs = cache["k"], cache["v"], cache["k_scale"], cache["v_scale"]
     lead = () if layers is None else (layers,)
-    if k.dim() != 4 + len(lead) or k.shape[:len(lead)] != lead:
-        raise SketchWalkError(f"cache k of shape {tuple(k.shape)}: {lead + ('n_pages', 'h_kv', 'B', 'd')} needed")
-    n_pages, h_kv, B, d = k.shape[-4:]
-    if v.shape != lead + (n_pages, h_kv, d, B):
-        raise SketchWalkError(f"cache v of shape {tuple(v.shape)} beside k of shape {tuple(k.shape)}")
-    for name, t in (("k_scale", ks), ("v_scale", vs)):
-        if t.shape != lead + (n_pages, h_kv):
-            raise SketchWalkError(f"cache {name} of shape {tuple(t.shape)} beside k of shape {tuple(k.shape)}")
-    _same_device(k.device, v, ks, vs)
-    return n_pages, h_kv, B, d, (_dev(k, "cache k", E4M3), _dev(v, "cache v", E4M3),
-                                 _dev(ks, "cache k_scale", torch.uint8), _dev(vs, "cache v_scale", torch.uint8))
-
-
-def _vec(t: torch.Tensor, n: int, name: str) -> int:
-    """A device int32 vector of n entries."""
-    p = _dev(t, name, torch.int32)
-    if t.numel() != n:
-        raise SketchWalkError(f"{name} has {t.numel()} entries, {n} needed")
-    return p
-
-
-def _mat(t: torch.Tensor, shape: tuple, name: str, dtype: torch.dtype = torch.int32) -> int:
-    p = _dev(t, name, dtype)
-    if tuple(t.shape) != shape:
-        raise SketchWalkError(f"{name} of shape {tuple(t.shape)}, {shape} needed")
-    return p
+    shape = k.shape
+    if len(shape) != 4 + len(lead) or shape[:-4] != lead:
+        raise SketchWalkError(f"cache k of shape {tuple(shape)}: {lead + ('n_pages', 'h_kv', 'B', 'd')} needed")
+    n_pages, h_kv, B, d = shape[-4:] if lead else shape
+    if v.shape != (*lead, n_pages, h_kv, d, B):
+        raise SketchWalkError(f"cache v of shape {tuple(v.shape)} beside k of shape {tuple(shape)}")
+    heads = (*lead, n_pages, h_kv)
+    if ks.shape != heads or vs.shape != heads:
+        raise SketchWalkError(f"cache k_scale, v_scale of shapes {tuple(ks.shape)}, {tuple(vs.shape)}: {heads} needed")
+    di = _gpu(k, "cache k")
+    return di, n_pages, h_kv, B, d, (_at(k, E4M3, di, "cache k"), _at(v, E4M3, di, "cache v"),
+                                     _at(ks, _U8, di, "cache k_scale"), _at(vs, _U8, di, "cache v_scale"))
 
 
 def block_tables(old_len: torch.Tensor, new_len: torch.Tensor, B: int, tables: torch.Tensor,
                  free_pages: torch.Tensor, n_free: torch.Tensor, n_slots: int, rows: int = 0,
-                 out: Optional[dict] = None) -> dict:
+                 out: Optional[dict] = None, workspace: Optional[torch.Tensor] = None) -> dict:
     """Brings ``tables`` [n][b_max] from the requests' old lengths to the new ones,
     with the stack of free pages (``free_pages`` [n_pages], its height ``n_free`` [1]);
     all int32, the last three updated in place. Returns dict with slots [n_slots],
     cu [n + 1], pos [n] and status [1] (0: done; otherwise nothing changed)."""
-    dev = tables.device
+    di = _gpu(tables, "tables")
     n, b_max = tables.shape
-    o = dict(out or {})
-    _fill(o, {"slots": (n_slots,), "cu": (n + 1,), "pos": (n,), "status": (1,)}, torch.int32, dev)
-    _same_device(dev, old_len, new_len, free_pages, n_free, *o.values())
-    with _on(dev):
-        rc = load().sw_block_tables(n, B, b_max, _vec(old_len, n, "old_len"), _vec(new_len, n, "new_len"),
-                                    _dev(tables, "tables", torch.int32),
-                                    _dev(free_pages, "free_pages", torch.int32), _vec(n_free, 1, "n_free"),
-                                    free_pages.numel(), rows, n_slots, _vec(o["slots"], n_slots, "slots"),
-                                    _vec(o["cu"], n + 1, "cu"), _vec(o["pos"], n, "pos"),
-                                    _vec(o["status"], 1, "status"), _stream(dev))
-    _check(rc, "sw_block_tables")
-    return o
+    p_old = _vec(old_len, n, di, "old_len")
+    o = out or {}
+    slots, cu, pos, status = o.get("slots"), o.get("cu"), o.get("pos"), o.get("status")
+    if slots is None:
+        slots = old_len.new_empty(n_slots)
+    if cu is None:
+        cu = old_len.new_empty(n + 1)
+    if pos is None:
+        pos = torch.empty_like(old_len)
+    if status is None:
+        status = old_len.new_empty(1)
+    lib = load()
+    wsb = lib.sw_block_tables_workspace_bytes(n, n_slots)
+    if wsb > 0 and (workspace is None or workspace.numel() < wsb):
+        workspace = old_len.new_empty(wsb, dtype=_U8)
+    p_ws, wsb = (None, 0) if workspace is None else (_at(workspace, _U8, di, "workspace"), workspace.numel())
+    _launch(di, lib.sw_block_tables, n, B, b_max, p_old, _vec(new_len, n, di, "new_len"),
+            _at(tables, _I32, di, "tables"), _at(free_pages, _I32, di, "free_pages"),
+            _vec(n_free, 1, di, "n_free"), free_pages.numel(), rows, n_slots, _vec(slots, n_slots, di, "slots"),
+            _vec(cu, n + 1, di, "cu"), _vec(pos, n, di, "pos"), _vec(status, 1, di, "status"), p_ws, wsb)
+    return {"slots": slots, "cu": cu, "pos": pos, "status": status}
 
 
 def kv_append_q8(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache: dict,
@@ -631,48 +654,41 @@ def kv_append_q8(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache: d
     """Writes k, v [h_kv][N][d] (bf16 or fp32; heads and tokens in any strides of whole
     16-byte pieces) into the pages of ``slots`` [N]. ``cu`` [n + 1] int32 (device): the
     tokens of a sequence together, in order; without it at most MAX_APPEND_TOKENS."""
-    n_pages, h_kv, B, d, pages = _pool(cache)
-    dev = cache["k"].device
-    _same_device(dev, k, v, slots, cu)
-    for name, t in (("k", k), ("v", v)):
-        if not t.is_cuda:
-            raise SketchWalkError(f"{name} must be a CUDA (HIP) tensor")
-        if t.dim() != 3 or t.shape[0] != h_kv or t.shape[2] != d or t.shape != k.shape:
-            raise SketchWalkError(f"{name} of shape {tuple(t.shape)}, ({h_kv}, N, {d}) needed")
-        if t.stride(2) != 1:
-            raise SketchWalkError(f"{name} must be contiguous in its last dimension")
-    if k.dtype != v.dtype:
+    di, n_pages, h_kv, B, d, pages = _pool(cache)
+    N = slots.numel()
+    shape = (h_kv, N, d)
+    if k.shape != shape or v.shape != shape:
+        raise SketchWalkError(f"k, v of shapes {tuple(k.shape)}, {tuple(v.shape)}: {shape} needed")
+    if k.get_device() != di or v.get_device() != di:
+        raise SketchWalkError(f"k, v on {k.device}, {v.device}, the cache on cuda:{di}")
+    if k.dtype is not v.dtype:
         raise SketchWalkError("k and v must share a dtype")
-    N = k.shape[1]
-    n = 0 if cu is None else cu.numel() - 1
-    with _on(dev):
-        rc = load().sw_kv_append_q8(_dtype_code(k), k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1),
-                                    v.stride(0), v.stride(1), N, n, _opt(cu, "cu", torch.int32),
-                                    _vec(slots, N, "slots"), n_pages, h_kv, d, B, *pages, _stream(dev))
-    _check(rc, "sw_kv_append_q8")
+    k_head, k_tok, k_dim = k.stride()
+    v_head, v_tok, v_dim = v.stride()
+    if k_dim != 1 or v_dim != 1:
+        raise SketchWalkError("k and v must be contiguous in their last dimension")
+    n, p_cu = (0, None) if cu is None else (cu.numel() - 1, _at(cu, _I32, di, "cu"))
+    _launch(di, load().sw_kv_append_q8, _dtype_code(k), k.data_ptr(), v.data_ptr(), k_head, k_tok, v_head,
+            v_tok, N, n, p_cu, _at(slots, _I32, di, "slots"), n_pages, h_kv, d, B, *pages)
 
 
 def kv_fetch_q8(cache: dict, tables: torch.Tensor, first: Optional[torch.Tensor], cu: torch.Tensor, N: int,
                 dtype: torch.dtype = torch.bfloat16, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None):
     """K, V [h_kv][N][d] in ``dtype``: positions first[s] .. (``first`` None: 0) of sequence
     s in rows cu[s] .. cu[s + 1] - 1 (device int32). Rows behind cu[n] are not written."""
-    n_pages, h_kv, B, d, pages = _pool(cache)
-    dev = cache["k"].device
+    di, n_pages, h_kv, B, d, pages = _pool(cache)
     n, b_max = tables.shape
     if out is None:
-        out = tuple(torch.empty((h_kv, N, d), dtype=dtype, device=dev) for _ in range(2))
-    K, V = out
-    for name, t in (("K", K), ("V", V)):
-        if tuple(t.shape) != (h_kv, N, d):
-            raise SketchWalkError(f"{name} of shape {tuple(t.shape)}, ({h_kv}, {N}, {d}) needed")
-    _same_device(dev, tables, first, cu, K, V)
-    with _on(dev):
-        rc = load().sw_kv_fetch_q8(_dtype_code(K), *pages, n_pages, h_kv, d, B, n, b_max,
-                                   _dev(tables, "tables", torch.int32),
-                                   None if first is None else _vec(first, n, "first"),
-                                   _vec(cu, n + 1, "cu"), N, _dev(K, "K"), _dev(V, "V", K.dtype),
-                                   _stream(dev))
-    _check(rc, "sw_kv_fetch_q8")
+        K = torch.empty((h_kv, N, d), dtype=dtype, device=tables.device)
+        V = torch.empty_like(K)
+    else:
+        K, V = out
+        _shaped(K, (h_kv, N, d), "K")
+        _shaped(V, (h_kv, N, d), "V")
+    dt = K.dtype
+    _launch(di, load().sw_kv_fetch_q8, _dtype_code(K), *pages, n_pages, h_kv, d, B, n, b_max,
+            _at(tables, _I32, di, "tables"), None if first is None else _vec(first, n, di, "first"),
+            _vec(cu, n + 1, di, "cu"), N, _at(K, dt, di, "K"), _at(V, dt, di, "V"))
     return K, V
 
 
@@ -689,27 +705,26 @@ def sparse_attn_decode_q8(q: torch.Tensor, cache: dict, tables: torch.Tensor, po
                           workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """sparse_attn_decode over a paged 8-bit cache: q [batch][h_q][d], tables
     [batch][b_max], idx [batch][kmax]."""
-    n_pages, h_kv, B, d, pages = _pool(cache)
+    di, n_pages, h_kv, B, d, pages = _pool(cache)
     batch, h_q, dq = q.shape
     if dq != d:
         raise SketchWalkError(f"q has head dimension {dq}, the cache {d}")
-    if tables.dim() != 2 or tables.shape[0] != batch:
+    rows, b_max = tables.shape
+    if rows != batch:
         raise SketchWalkError(f"tables of shape {tuple(tables.shape)}, ({batch}, b_max) needed")
-    dev = q.device
+    dt = q.dtype
     if O is None:
         O = torch.empty_like(q)
+    else:
+        _shaped(O, (batch, h_q, d), "O")
+    _shaped(idx, (batch, kmax), "idx")
     wsb = decode_attn_q8_workspace_bytes(batch, h_q, h_kv, d)
     if workspace is None or workspace.numel() < wsb:
-        workspace = torch.empty((wsb,), dtype=torch.uint8, device=dev)
-    _same_device(dev, cache["k"], tables, pos, idx, cnt, O, workspace)
-    with _on(dev):
-        rc = load().sw_sparse_attn_decode_q8(
-            _dtype_code(q), _dev(q, "q"), *pages, batch, h_q, h_kv, d, n_pages,
-            _dev(tables, "tables", torch.int32), tables.shape[1], B, _vec(pos, batch, "pos"),
-            _mat(idx, (batch, kmax), "idx"), _vec(cnt, batch, "cnt"), kmax, float(scale),
-            _mat(O, (batch, h_q, d), "O", q.dtype), _dev(workspace, "workspace", torch.uint8),
-            workspace.numel(), _stream(dev))
-    _check(rc, "sw_sparse_attn_decode_q8")
+        workspace = q.new_empty(wsb, dtype=_U8)
+    _launch(di, load().sw_sparse_attn_decode_q8, _dtype_code(q), _at(q, dt, di, "q"), *pages, batch, h_q, h_kv,
+            d, n_pages, _at(tables, _I32, di, "tables"), b_max, B, _vec(pos, batch, di, "pos"),
+            _at(idx, _I32, di, "idx"), _vec(cnt, batch, di, "cnt"), kmax, float(scale), _at(O, dt, di, "O"),
+            _at(workspace, _U8, di, "workspace"), workspace.numel())
     return O
 
 
@@ -723,37 +738,40 @@ def decode_step_q8(q_new: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor
     ``slots`` [batch] (block_tables with rows=1), the attention reads through ``tables``
     [batch][b_max]. Returns what decode_step returns."""
     L, batch, h_q, d = q_new.shape
-    n_pages, h_kv, B, dc, pages = _pool(cache, L)
+    di, n_pages, h_kv, B, dc, pages = _pool(cache, L)
     dev = q_new.device
-    if dc != d or tuple(k_new.shape) != (L, batch, h_kv, d) or v_new.shape != k_new.shape:
-        raise SketchWalkError(f"k_new, v_new of shape {tuple(k_new.shape)}, {tuple(v_new.shape)}: "
-                              f"({L}, {batch}, {h_kv}, {dc}) needed")
-    if tables.dim() != 2 or tables.shape[0] != batch:
+    if dc != d:
+        raise SketchWalkError(f"q_new has head dimension {d}, the cache {dc}")
+    _shaped(k_new, (L, batch, h_kv, d), "k_new")
+    _shaped(v_new, (L, batch, h_kv, d), "v_new")
+    n, b_max = tables.shape
+    if n != batch:
         raise SketchWalkError(f"tables of shape {tuple(tables.shape)}, ({batch}, b_max) needed")
-    b_max, r = tables.shape[1], int(cols.numel())
+    r = int(cols.numel())
+    _shaped(signs, (d,), "signs")
     if kmax is None:
         kmax = select_max_count_decode(b_max, k=k, density_pct=density_pct, flags=flags)
-    if state.numel() != L * decode_state_bytes(batch, d, r, b_max):
-        raise SketchWalkError(f"state of {state.numel()} bytes, {L} * {decode_state_bytes(batch, d, r, b_max)} needed")
+    need = L * decode_state_bytes(batch, d, r, b_max)
+    if state.numel() != need:
+        raise SketchWalkError(f"state of {state.numel()} bytes, {need} needed")
+    shapes = {"rows": (L, batch, b_max), "idx": (L, batch, kmax), "cnt": (L, batch), "O": (L, batch, h_q, d)}
     o = dict(out or {})
-    _fill(o, {"rows": (L, batch, b_max)}, torch.float64, dev)
-    _fill(o, {"idx": (L, batch, kmax), "cnt": (L, batch)}, torch.int32, dev)
+    _fill(o, {"rows": shapes["rows"]}, torch.float64, dev)
+    _fill(o, {"idx": shapes["idx"], "cnt": shapes["cnt"]}, _I32, dev)
     if "O" not in o:
         o["O"] = torch.empty_like(q_new)
+    for name, shape in shapes.items():
+        _shaped(o[name], shape, name)
     least = decode_attn_q8_workspace_bytes(batch, h_q, h_kv, d)
     if workspace is None or workspace.numel() < least:
         wsb = int(load().sw_decode_step_q8_workspace_bytes(batch, h_q, h_kv, d))
-        workspace = torch.empty((wsb,), dtype=torch.uint8, device=dev)
-    _same_device(dev, k_new, v_new, cache["k"], tables, slots, state, pos, signs, cols, workspace, *o.values())
-    with _on(dev):
-        rc = load().sw_decode_step_q8(
-            _dtype_code(q_new), L, batch, h_q, h_kv, d, r, n_pages, B, b_max, _dev(q_new, "q_new"),
-            _dev(k_new, "k_new", q_new.dtype), _dev(v_new, "v_new", q_new.dtype), *pages,
-            _dev(tables, "tables", torch.int32), _vec(slots, batch, "slots"),
-            _dev(state, "state", torch.uint8), _vec(pos, batch, "pos"), _mat(signs, (d,), "signs", torch.int8),
-            _dev(cols, "cols", torch.int32), s, walk_variant, k, density_pct, flags, kmax, float(scale),
-            _mat(o["rows"], (L, batch, b_max), "rows", torch.float64), _mat(o["idx"], (L, batch, kmax), "idx"),
-            _mat(o["cnt"], (L, batch), "cnt"), _mat(o["O"], (L, batch, h_q, d), "O", q_new.dtype),
-            _dev(workspace, "workspace", torch.uint8), workspace.numel(), _stream(dev))
-    _check(rc, "sw_decode_step_q8")
+        workspace = q_new.new_empty(wsb, dtype=_U8)
+    dt = q_new.dtype
+    _launch(di, load().sw_decode_step_q8, _dtype_code(q_new), L, batch, h_q, h_kv, d, r, n_pages, B, b_max,
+            _at(q_new, dt, di, "q_new"), _at(k_new, dt, di, "k_new"), _at(v_new, dt, di, "v_new"), *pages,
+            _at(tables, _I32, di, "tables"), _vec(slots, batch, di, "slots"), _at(state, _U8, di, "state"),
+            _vec(pos, batch, di, "pos"), _at(signs, torch.int8, di, "signs"), _at(cols, _I32, di, "cols"), s,
+            walk_variant, k, density_pct, flags, kmax, float(scale), _at(o["rows"], torch.float64, di, "rows"),
+            _at(o["idx"], _I32, di, "idx"), _at(o["cnt"], _I32, di, "cnt"), _at(o["O"], dt, di, "O"),
+            _at(workspace, _U8, di, "workspace"), workspace.numel())
     return o

@@ -586,10 +586,19 @@ static int check_pages(const void* k_pages, const void* v_pages, const uint8_t* 
   return SW_OK;
 }
 
+int64_t sw_block_tables_workspace_bytes(int n_seqs, int64_t n_slots) {
+  if (n_seqs < 1 || n_seqs > 65536 || n_slots < 0 || n_slots >= (int64_t)1 << 31) {
+    fail(SW_ERR_INVALID_ARG, "n_seqs=%d n_slots=%lld", n_seqs, (long long)n_slots);
+    return -1;
+  }
+  ok();
+  return sw::block_tables_workspace_bytes(n_seqs, n_slots);
+}
+
 int sw_block_tables(int n_seqs, int B, int b_max, const int32_t* old_len, const int32_t* new_len,
                     int32_t* tables, int32_t* free_pages, int32_t* n_free, int n_pages, int rows,
                     int64_t n_slots, int32_t* slots, int32_t* cu_seqlens, int32_t* pos,
-                    int32_t* status, void* stream) {
+                    int32_t* status, void* workspace, int64_t workspace_bytes, void* stream) {
   if (n_seqs < 1 || n_seqs > 65536) return fail(SW_ERR_INVALID_ARG, "n_seqs=%d outside [1, 65536]", n_seqs);
   CHECK(check_pool(n_pages, 1, 64, B));
   if (b_max < 1 || (int64_t)b_max * B >= (int64_t)1 << 31)
@@ -609,8 +618,16 @@ int sw_block_tables(int n_seqs, int B, int b_max, const int32_t* old_len, const 
   CHECK(check_ptr(cu_seqlens, 4, "cu_seqlens"));
   CHECK(check_ptr(pos, 4, "pos"));
   CHECK(check_ptr(status, 4, "status"));
+  const int64_t need = sw::block_tables_workspace_bytes(n_seqs, n_slots);
+  if (need > 0) {
+    CHECK(check_ptr(workspace, 8, "workspace"));
+    if (workspace_bytes < need)
+      return fail(SW_ERR_INVALID_ARG, "workspace_bytes=%lld < required %lld",
+                  (long long)workspace_bytes, (long long)need);
+  }
   hipError_t e = sw::launch_block_tables(n_seqs, B, b_max, old_len, new_len, tables, free_pages, n_free,
                                          n_pages, rows, (int)n_slots, slots, cu_seqlens, pos, status,
+                                         static_cast<int32_t*>(workspace),
                                          reinterpret_cast<hipStream_t>(stream));
   return hip_status(e, "sw_block_tables launch");
 }
@@ -628,6 +645,11 @@ int sw_kv_append_q8(int dtype, const void* k, const void* v, int64_t k_head_stri
   if (!cu_seqlens && N > SW_MAX_APPEND_TOKENS)
     return fail(SW_ERR_UNSUPPORTED, "N=%lld tokens without cu_seqlens, at most %d", (long long)N,
                 SW_MAX_APPEND_TOKENS);
+  // a launch holds less than 2^32 threads
+  const int64_t wgs = (cu_seqlens ? N / B + 2ll * n_seqs : N) * 2 * h_kv;
+  if (wgs >= (int64_t)1 << 24)
+    return fail(SW_ERR_UNSUPPORTED, "N=%lld tokens of %d sequences and %d heads: too many for one call",
+                (long long)N, cu_seqlens ? n_seqs : 0, h_kv);
   const int64_t strides[4] = {k_head_stride, k_token_stride, v_head_stride, v_token_stride};
   const int piece = dtype == SW_BF16 ? 8 : 4;
   for (int64_t x : strides)
@@ -661,6 +683,8 @@ int sw_kv_fetch_q8(int dtype, const void* k_pages, const void* v_pages, const ui
   CHECK(check_ptr(cu_seqlens, 4, "cu_seqlens"));
   if (first && !aligned(first, 4)) return fail(SW_ERR_INVALID_ARG, "first misaligned");
   if (N == 0) return ok();
+  if (N / 64 + 2ll * n_seqs >= (int64_t)1 << 24)   // a launch holds less than 2^32 threads
+    return fail(SW_ERR_UNSUPPORTED, "N=%lld tokens of %d sequences: too many for one call", (long long)N, n_seqs);
   CHECK(check_ptr(K, 16, "K"));
   CHECK(check_ptr(V, 16, "V"));
   hipError_t e = sw::launch_kv_fetch_q8(dtype, k_pages, v_pages, k_scale, v_scale, n_pages, h_kv, d, B,

@@ -3,7 +3,7 @@
 //
 //  block_tables_kernel  pages of requests that end back onto the free stack,
 //                       pages for new blocks off it, the new tokens' slots
-//  slots_kernel         the slots alone, for calls with many of them
+//  spread_kernel        pages and slots of calls with many of them
 //  kv_append_q8_kernel  new tokens into the pages their slots name
 //  kv_fetch_q8_kernel   tokens of the cache back as bf16 or fp32
 #include <type_traits>
@@ -55,18 +55,28 @@ __device__ __forceinline__ int slot_of(const int32_t* table, int p, int B, int n
   return (unsigned)page < (unsigned)n_pages ? page * B + (p - j * B) : -1;
 }
 
-// One workgroup. In order: every length is checked and the pages to give back
-// (R) and to take (A) are counted; then, if the call can be served whole, the
-// R released pages go onto the stack so that the first of them (sequences
-// ascending, blocks ascending) is on top, and the A new blocks take pages from
-// the top in the same order. Bounded by latency: four dependent loads and a
-// dozen barriers.
+// What the workgroups of a spread call need of the plan: the pages that the
+// sequences before each one give back and take, and the stack.
+struct TabPlan {
+  int32_t* rel;       // [n_seqs + 1]
+  int32_t* alc;       // [n_seqs + 1]
+  int32_t* head;      // [2]: whether the call is served, height of the stack before it
+};
+
+// One workgroup. Every length is checked and the pages to give back (R) and to
+// take (A) are counted. If the call can be served whole, the R released pages go
+// onto the stack so that the first of them (sequences ascending, blocks
+// ascending) is on top, and the A new blocks take pages from the top in the same
+// order. Bounded by latency, four dependent loads and a dozen barriers: 4.3 us for
+// one token more for each of 64 requests. PLAN: the prefixes alone, for
+// spread_kernel: pages moved by one workgroup take 1.5 us per 1024, slots as
+// much.
+template <bool PLAN>
 __global__ __launch_bounds__(kTabThreads) void block_tables_kernel(
     int n_seqs, int B, int b_max, const int32_t* __restrict__ old_len,
     const int32_t* __restrict__ new_len, int32_t* __restrict__ tables, int32_t* __restrict__ free_pages,
-    int32_t* __restrict__ n_free, int n_pages, int rows, int n_slots, int slots_here,
-    int32_t* __restrict__ slots, int32_t* __restrict__ cu, int32_t* __restrict__ pos,
-    int32_t* __restrict__ status) {
+    int32_t* __restrict__ n_free, int n_pages, int rows, int n_slots, int32_t* __restrict__ slots,
+    int32_t* __restrict__ cu, int32_t* __restrict__ pos, int32_t* __restrict__ status, TabPlan plan) {
   __shared__ int tmp[kTabThreads / 64];
   __shared__ int pre[kTabThreads], first[kTabThreads];
   __shared__ long long sums[3];
@@ -99,42 +109,50 @@ __global__ __launch_bounds__(kTabThreads) void block_tables_kernel(
   const bool valid = !bad && nf >= 0 && nf + R <= n_pages && (rows > 0 || sums[2] <= n_slots);
   const bool ok = valid && A - R <= nf;
   const int top = nf + (int)R;                     // of the stack, after the releases
-  if (t == 0) *status = valid ? (ok ? 0 : 1) : 2;
-
-  int done_r = 0, done_a = 0, done_g = 0;
-  for (int phase = 0; phase < 2 && ok; ++phase) {
-    // 0: releases; 1: allocations
-    if (phase == 0 ? R == 0 : A == 0) continue;
-    for (int s0 = 0; s0 < n_seqs; s0 += kTabThreads) {
-      const int s = s0 + t;
-      int has = 0, need = 0;
-      if (s < n_seqs) {
-        has = (int)((old_len[s] + (long long)B - 1) / B);
-        need = (int)((new_len[s] + (long long)B - 1) / B);
-      }
-      int total;
-      const int k0 = tab_scan(phase == 0 ? max(has - need, 0) : max(need - has, 0), tmp, &total);
-      pre[t] = k0;
-      first[t] = phase == 0 ? need : has;
-      __syncthreads();
-      const int base = phase == 0 ? done_r : done_a;
-      for (int k = t; k < total; k += kTabThreads) {
-        const int i = last_at_most(pre, kTabThreads, k);
-        int32_t* entry = tables + (long long)(s0 + i) * b_max + first[i] + (k - pre[i]);
-        int32_t* item = free_pages + (top - 1 - (base + k));
-        if (phase == 0) {
-          *item = *entry;
-          *entry = -1;
-        } else {
-          *entry = *item;
-        }
-      }
-      if (phase == 0) done_r += total; else done_a += total;
-      __syncthreads();
+  if (t == 0) {
+    *status = valid ? (ok ? 0 : 1) : 2;
+    if (ok) *n_free = top - (int)A;
+    if (PLAN) {
+      plan.head[0] = ok;
+      plan.head[1] = nf;
     }
   }
-  if (t == 0 && ok) *n_free = top - (int)A;
-  // cumulative new tokens, positions of the last ones
+  if (!PLAN) {
+    int done_r = 0, done_a = 0;
+    for (int phase = 0; phase < 2 && ok; ++phase) {
+      // 0: releases; 1: allocations
+      if (phase == 0 ? R == 0 : A == 0) continue;
+      for (int s0 = 0; s0 < n_seqs; s0 += kTabThreads) {
+        const int s = s0 + t;
+        int has = 0, need = 0;
+        if (s < n_seqs) {
+          has = (int)((old_len[s] + (long long)B - 1) / B);
+          need = (int)((new_len[s] + (long long)B - 1) / B);
+        }
+        int total;
+        const int k0 = tab_scan(phase == 0 ? max(has - need, 0) : max(need - has, 0), tmp, &total);
+        pre[t] = k0;
+        first[t] = phase == 0 ? need : has;
+        __syncthreads();
+        const int base = phase == 0 ? done_r : done_a;
+        for (int k = t; k < total; k += kTabThreads) {
+          const int i = last_at_most(pre, kTabThreads, k);
+          int32_t* entry = tables + (long long)(s0 + i) * b_max + first[i] + (k - pre[i]);
+          int32_t* item = free_pages + (top - 1 - (base + k));
+          if (phase == 0) {
+            *item = *entry;
+            *entry = -1;
+          } else {
+            *entry = *item;
+          }
+        }
+        if (phase == 0) done_r += total; else done_a += total;
+        __syncthreads();
+      }
+    }
+  }
+  // cumulative new tokens (and pages), positions of the last ones
+  int done_g = 0, done_r = 0, done_a = 0;
   for (int s0 = 0; s0 < n_seqs; s0 += kTabThreads) {
     const int s = s0 + t;
     const int o = s < n_seqs ? old_len[s] : 0, w = s < n_seqs ? new_len[s] : 0;
@@ -145,9 +163,24 @@ __global__ __launch_bounds__(kTabThreads) void block_tables_kernel(
       pos[s] = (ok ? w : o) - 1;
     }
     done_g += total;
+    if (PLAN) {
+      const int more = ok ? (int)((w + (long long)B - 1) / B) - (int)((o + (long long)B - 1) / B) : 0;
+      const int r0 = tab_scan(max(-more, 0), tmp, &total);
+      if (s < n_seqs) plan.rel[s] = done_r + r0;
+      done_r += total;
+      const int a0 = tab_scan(max(more, 0), tmp, &total);
+      if (s < n_seqs) plan.alc[s] = done_a + a0;
+      done_a += total;
+    }
   }
-  if (t == 0) cu[n_seqs] = done_g;
-  if (!slots_here) return;
+  if (t == 0) {
+    cu[n_seqs] = done_g;
+    if (PLAN) {
+      plan.rel[n_seqs] = done_r;
+      plan.alc[n_seqs] = done_a;
+    }
+  }
+  if (PLAN) return;
   __syncthreads();                                 // tables and cu as written above
   for (int x = t; x < n_slots; x += kTabThreads) {
     int v = -1;
@@ -163,44 +196,101 @@ __global__ __launch_bounds__(kTabThreads) void block_tables_kernel(
   }
 }
 
-// Slots of calls with many new tokens: thread x takes four of them.
-__global__ __launch_bounds__(256) void slots_kernel(int n_seqs, int B, int b_max,
-                                                    const int32_t* __restrict__ old_len,
-                                                    const int32_t* __restrict__ new_len,
-                                                    const int32_t* __restrict__ tables, int n_pages,
-                                                    int rows, int n_slots, const int32_t* __restrict__ cu,
-                                                    const int32_t* __restrict__ status,
-                                                    int32_t* __restrict__ slots) {
-  const bool ok = *status == 0;
-  const int total = cu[n_seqs];
-  for (int e = 0; e < 4; ++e) {
-    const long long x = ((long long)blockIdx.x * 256 + threadIdx.x) * 4 + e;
-    if (x >= n_slots) return;
-    int v = -1;
-    if (rows > 0) {
-      const int s = (int)(x / rows), i = (int)(x - (long long)s * rows);
-      const int o = old_len[s];
-      if (ok && i < new_len[s] - o) v = slot_of(tables + (long long)s * b_max, o + i, B, n_pages);
-    } else if (x < total) {
-      const int s = last_at_most(cu, n_seqs, (int)x);
-      v = slot_of(tables + (long long)s * b_max, old_len[s] + ((int)x - cu[s]), B, n_pages);
-    }
-    slots[x] = v;
+constexpr int kSpreadLds = 2048;                   // prefixes kept in LDS
+
+// Pages and slots of a planned call over many workgroups. 16 lanes take the page
+// of rank k, from the k-th block given back, or off the stack where there is
+// none, and put it into the k-th new block and that block's slots, or onto the
+// stack where there is none: no workgroup reads what another one writes. Slots of
+// the blocks that the sequences had before, and those that stay empty, are
+// written per sequence and behind the last.
+__global__ __launch_bounds__(256) void spread_kernel(
+    int n_seqs, int B, int b_max, const int32_t* __restrict__ old_len,
+    const int32_t* __restrict__ new_len, int32_t* __restrict__ tables, int32_t* __restrict__ free_pages,
+    int n_pages, int rows, int n_slots, int32_t* __restrict__ slots, const int32_t* __restrict__ cu,
+    TabPlan plan) {
+  __shared__ int rel[kSpreadLds], alc[kSpreadLds];
+  const int t = threadIdx.x, lane = t & 15;
+  const int unit0 = blockIdx.x * 16 + (t >> 4), units = gridDim.x * 16;
+  const long long x0 = (long long)blockIdx.x * 256 + t, xs = (long long)gridDim.x * 256;
+  if (!plan.head[0]) {
+    for (long long x = x0; x < n_slots; x += xs) slots[x] = -1;
+    return;
   }
+  const int nf = plan.head[1], R = plan.rel[n_seqs], A = plan.alc[n_seqs];
+  const bool lds = n_seqs <= kSpreadLds;
+  if (lds)
+    for (int s = t; s < n_seqs; s += 256) {
+      rel[s] = plan.rel[s];
+      alc[s] = plan.alc[s];
+    }
+  __syncthreads();
+  for (int k = unit0; k < max(R, A); k += units) {
+    int page;
+    if (k < R) {
+      const int s = lds ? last_at_most(rel, n_seqs, k) : last_at_most(plan.rel, n_seqs, k);
+      const int need = (int)((new_len[s] + (long long)B - 1) / B);
+      int32_t* entry = tables + (long long)s * b_max + need + (k - plan.rel[s]);
+      page = *entry;
+      // every lane has the page before one of them clears the entry
+      page = __shfl(page, t & 48);
+      if (lane == 0) *entry = -1;
+    } else {
+      page = free_pages[nf - 1 - (k - R)];
+    }
+    if (k >= A) {
+      if (lane == 0) free_pages[nf + R - 1 - k] = page;
+      continue;
+    }
+    const int s = lds ? last_at_most(alc, n_seqs, k) : last_at_most(plan.alc, n_seqs, k);
+    const int o = old_len[s], w = new_len[s];
+    const int j = (int)((o + (long long)B - 1) / B) + (k - plan.alc[s]);
+    if (lane == 0) tables[(long long)s * b_max + j] = page;
+    const bool have = (unsigned)page < (unsigned)n_pages;
+    const long long out = (rows > 0 ? (long long)s * rows : cu[s]) + ((long long)j * B - o);
+    const int n = min(B, w - j * B);
+    for (int i = lane; i < n; i += 16) slots[out + i] = have ? page * B + i : -1;
+  }
+  for (int s = unit0; s < n_seqs; s += units) {
+    const int o = old_len[s], w = new_len[s];
+    const long long out = rows > 0 ? (long long)s * rows : cu[s];
+    const int end = (int)min((long long)w, (o + (long long)B - 1) / B * B);   // of the block it had
+    if (o < end) {
+      const int j = o / B;
+      const int page = tables[(long long)s * b_max + j];
+      const bool have = (unsigned)page < (unsigned)n_pages;
+      for (int p = o + lane; p < end; p += 16) slots[out + p - o] = have ? page * B + (p - j * B) : -1;
+    }
+    for (int i = max(w - o, 0) + lane; i < rows; i += 16) slots[out + i] = -1;
+  }
+  if (rows == 0)
+    for (long long x = cu[n_seqs] + x0; x < n_slots; x += xs) slots[x] = -1;
+}
+
+// Calls with few slots are one launch. (Many pages given back by such a call are
+// moved by its one workgroup.)
+constexpr long long kTabOneLaunch = 4 * kTabThreads;
+
+int64_t block_tables_workspace_bytes(int n_seqs, int64_t n_slots) {
+  return n_slots <= kTabOneLaunch ? 0 : 8ll * (n_seqs + 2);
 }
 
 hipError_t launch_block_tables(int n_seqs, int B, int b_max, const int32_t* old_len,
                                const int32_t* new_len, int32_t* tables, int32_t* free_pages,
                                int32_t* n_free, int n_pages, int rows, int n_slots, int32_t* slots,
-                               int32_t* cu, int32_t* pos, int32_t* status, hipStream_t st) {
-  const int here = n_slots <= 8 * kTabThreads;
-  hipLaunchKernelGGL(block_tables_kernel, dim3(1), dim3(kTabThreads), 0, st, n_seqs, B, b_max, old_len,
-                     new_len, tables, free_pages, n_free, n_pages, rows, n_slots, here, slots, cu, pos,
-                     status);
-  if (!here)
-    hipLaunchKernelGGL(slots_kernel, dim3((unsigned)((n_slots + 1023ll) / 1024)), dim3(256), 0, st,
-                       n_seqs, B, b_max, old_len, new_len, tables, n_pages, rows, n_slots, cu, status,
-                       slots);
+                               int32_t* cu, int32_t* pos, int32_t* status, int32_t* ws, hipStream_t st) {
+  if (n_slots <= kTabOneLaunch) {
+    hipLaunchKernelGGL(block_tables_kernel<false>, dim3(1), dim3(kTabThreads), 0, st, n_seqs, B, b_max,
+                       old_len, new_len, tables, free_pages, n_free, n_pages, rows, n_slots, slots, cu,
+                       pos, status, TabPlan{});
+    return hipGetLastError();
+  }
+  const TabPlan plan{ws, ws + n_seqs + 1, ws + 2 * (n_seqs + 1)};
+  hipLaunchKernelGGL(block_tables_kernel<true>, dim3(1), dim3(kTabThreads), 0, st, n_seqs, B, b_max,
+                     old_len, new_len, tables, free_pages, n_free, n_pages, rows, n_slots, slots, cu, pos,
+                     status, plan);
+  hipLaunchKernelGGL(spread_kernel, dim3(1024), dim3(256), 0, st, n_seqs, B, b_max, old_len, new_len,
+                     tables, free_pages, n_pages, rows, n_slots, slots, cu, plan);
   return hipGetLastError();
 }
 
@@ -208,196 +298,297 @@ hipError_t launch_block_tables(int n_seqs, int B, int b_max, const int32_t* old_
 // tokens into the cache
 // ---------------------------------------------------------------------------
 
-template <typename T>
-__device__ __forceinline__ float q8_load(const T* p) {
-  if constexpr (sizeof(T) == 2)
-    return bf16_to_f32(*p);
-  else
-    return *p;
-}
-
 // The part of a sequence's tokens that lies in one block. Workgroup w of
 // floor(N / B) + 2 n_seqs finds its own: sequence s has the workgroups from
 // cu[s] / B + 2 s on, which is enough for its floor(n / B) + 2 blocks at most
-// however it lies in them, so no prefix of block counts is needed.
-__device__ __forceinline__ int seq_of_wg(int w, int n_seqs, const int32_t* cu, int B) {
-  int count = 0;
-  for (int s0 = 0; s0 < n_seqs; s0 += 256) {
-    const int s = s0 + threadIdx.x;
-    const int c = __syncthreads_count(s < n_seqs && (long long)cu[min(s, n_seqs)] / B + 2ll * s <= w);
-    count += c;
-    if (c < 256) break;
+// however it lies in them, so no prefix of block counts is needed. Returns the
+// block's number in the sequence's stretch; c0, c1 are the stretch's tokens.
+__device__ __forceinline__ long long seq_of_wg(int w, int n_seqs, const int32_t* cu, int B, int N,
+                                               int* s_out, int* c0, int* c1) {
+  __shared__ int mine[3];
+  const int t = threadIdx.x;
+  if (t == 0) mine[0] = 0, mine[1] = mine[2] = 0;
+  __syncthreads();
+  for (int s0 = 0; s0 < n_seqs; s0 += blockDim.x) {
+    const int s = s0 + t;
+    const int a = cu[min(s, n_seqs)], b = cu[min(s + 1, n_seqs)];
+    // the last sequence that starts at or before w
+    if (s < n_seqs && a / B + 2ll * s <= w && (s + 1 == n_seqs || b / B + 2ll * (s + 1) > w)) {
+      mine[0] = s;
+      mine[1] = a;
+      mine[2] = b;
+    }
   }
-  return max(count - 1, 0);
+  __syncthreads();
+  *s_out = mine[0];
+  *c0 = max(mine[1], 0);
+  *c1 = min(mine[2], N);
+  return w - (*c0 / B + 2ll * *s_out);
 }
 
-constexpr int kQ8Tile = 64;                        // tokens transposed at a time
-constexpr int kQ8Stride = kQ8Tile + 4;             // bytes from one dimension's row to the next
+// Tokens of a block that an append workgroup holds in registers at a time: 64 KB,
+// or the whole block if it is smaller. A multiple of 16.
+__host__ __device__ constexpr int q8_part(int B, int d, int size) {
+  const int most = 65536 / (d * size);
+  return B < most ? B : most;
+}
 
-// One workgroup per (block with new tokens, head). With cu the block's tokens
-// are a stretch of one sequence's; without, a workgroup per token collects all
-// tokens of its page and leaves the work to the first of them.
-//   amax    over the new tokens' finite values, K and V apart
+typedef unsigned int u32x4f __attribute__((ext_vector_type(4)));
+typedef unsigned short u16x2q __attribute__((ext_vector_type(2)));
+typedef short s16x2q __attribute__((ext_vector_type(2)));
+
+// The elements of a word of two bf16 or one fp32 as magnitudes, by their bits
+// (which order as the numbers do; infinity and NaN come last).
+template <typename T>
+struct Q8Word;
+template <>
+struct Q8Word<uint16_t> {
+  static constexpr uint32_t kInf = 0x7f80u;
+  u16x2q m = {0, 0};
+  __device__ void add(uint32_t w) {
+    m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2q, w & 0x7fff7fffu));
+  }
+  __device__ uint32_t largest() const { return m[0] > m[1] ? m[0] : m[1]; }
+  __device__ static float value(uint32_t bits) { return __uint_as_float(bits << 16); }
+  // finite elements only; infinities become NaN in w
+  __device__ void add_finite(uint32_t& w) {
+#pragma unroll
+    for (int h = 0; h < 32; h += 16) {
+      const uint32_t x = w >> h & 0x7fffu;
+      if (x < kInf) add(x);
+      else w |= 0x40u << h;
+    }
+  }
+  // codes of the word's elements / scale in one half of `old`
+  template <bool HI>
+  __device__ static uint32_t codes(uint32_t old, uint32_t w, uint32_t, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(
+        __builtin_bit_cast(s16x2q, old), __builtin_bit_cast(bf16x2q, w), scale, HI));
+  }
+};
+template <>
+struct Q8Word<float> {
+  static constexpr uint32_t kInf = 0x7f800000u;
+  uint32_t m = 0;
+  __device__ void add(uint32_t w) { m = max(m, w & 0x7fffffffu); }
+  __device__ uint32_t largest() const { return m; }
+  __device__ static float value(uint32_t bits) { return __uint_as_float(bits); }
+  __device__ void add_finite(uint32_t& w) {
+    const uint32_t x = w & 0x7fffffffu;
+    if (x < kInf) add(x);
+    else w |= 0x400000u;
+  }
+  // codes of two words
+  template <bool HI>
+  __device__ static uint32_t codes(uint32_t old, uint32_t w, uint32_t w2, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(
+        __builtin_bit_cast(s16x2q, old), __uint_as_float(w), __uint_as_float(w2), scale, HI));
+  }
+};
+
+// One workgroup per (block with new tokens, head, keys or values). SEQ: the
+// block's tokens are a stretch of one sequence's. Otherwise a workgroup per token
+// collects all tokens of its page and leaves the work to the first of them.
+//   amax    over the new tokens' finite values, by their bits: not finite is the
+//           largest, and only a block that has such a value looks at each
 //   scale   of those alone if the block's first token is among them, else the
 //           larger of the block's own and theirs; in the latter case the
 //           block's codes are rounded again if the scale grew
-//   codes   K rows as they are, V through LDS: 16 tokens of a dimension are one
-//           16-byte store where all of them are new
-template <typename T>
-__global__ __launch_bounds__(256) void kv_append_q8_kernel(
+//   codes   keys row by row; values four tokens of a dimension at a time into
+//           LDS and from there, 16 tokens of a dimension in one store where all
+//           of them are new
+// A thread takes 16 bytes of each of four consecutive rows and keeps them from the
+// maximum to the codes (blocks over 64 KB are read twice), so the workgroup's
+// size goes by the block's: 1024 threads at 64 KB (256 threads with four such
+// pieces each need 250 registers, which halves the wavefronts).
+template <typename T, int D, bool SEQ>
+__global__ __launch_bounds__(1024) void kv_append_q8_kernel(
     const T* __restrict__ k, const T* __restrict__ v, TokenStrides sd, int N, int n_seqs,
-    const int32_t* __restrict__ cu, const int32_t* __restrict__ slots, int n_pages, int h_kv, int d,
-    int B, uint8_t* __restrict__ Kp, uint8_t* __restrict__ Vp, uint8_t* __restrict__ ks,
+    const int32_t* __restrict__ cu, const int32_t* __restrict__ slots, int n_pages, int h_kv, int B,
+    uint8_t* __restrict__ Kp, uint8_t* __restrict__ Vp, uint8_t* __restrict__ ks,
     uint8_t* __restrict__ vs) {
-  __shared__ int map[1024];                        // token of each place in the block, -1: none
-  __shared__ float red[2][4];
-  __shared__ __attribute__((aligned(16))) uint8_t tile[256 * kQ8Stride];
-  __shared__ int leader;
-  const int t = threadIdx.x, g = blockIdx.y;
-  const long long layer = blockIdx.z;
-  k += layer * sd.layer;
-  v += layer * sd.layer;
-  const long long pool = (long long)n_pages * h_kv;
-  Kp += layer * pool * B * d;
-  Vp += layer * pool * B * d;
-  ks += layer * pool;
-  vs += layer * pool;
-  int i0, i1, slot;
-  if (cu) {
-    const int s = seq_of_wg(blockIdx.x, n_seqs, cu, B);
-    const int c0 = max(cu[s], 0), c1 = min(cu[s + 1], N);
-    if (c0 >= c1) return;
-    const int begin = slots[c0];
-    if (begin < 0) return;
-    const long long j = blockIdx.x - (c0 / B + 2ll * s);
-    const long long lo = c0 + j * B - begin % B;
-    i0 = (int)max((long long)c0, lo);
-    i1 = (int)min((long long)c1, lo + B);
-    if (i0 >= i1) return;
-    slot = slots[i0];
-  } else {
-    i0 = blockIdx.x;
-    i1 = N;
-    slot = slots[i0];
-  }
-  if (slot < 0) return;
-  const int page = slot / B, base = page * B;
-  if (page >= n_pages) return;
-  for (int o = t; o < B; o += 256) map[o] = -1;
-  if (t == 0) leader = 1;
-  __syncthreads();
-  if (!cu) {
-    for (int i = t; i < i0; i += 256)
-      if ((unsigned)(slots[i] - base) < (unsigned)B) leader = 0;
-  }
-  for (int i = i0 + t; i < i1; i += 256) {
-    const int o = slots[i] - base;
-    if ((unsigned)o < (unsigned)B) atomicMax(&map[o], i);
-  }
-  __syncthreads();
-  if (!leader) return;
-
+  using W = Q8Word<T>;
   constexpr int V = 16 / (int)sizeof(T);           // elements of a 16-byte piece
-  const int pieces = d / V;                        // of a row
-  const int per = 256 / pieces;                    // rows at a time
-  const int pc = t % pieces, row0 = t / pieces;
-  const T* kg = k + g * sd.k_head + pc * V;
-  const T* vg = v + g * sd.v_head + pc * V;
-  float ka = 0.0f, va = 0.0f;
-  if (row0 < per)
-    for (int o = row0; o < B; o += per) {
-      const int i = map[o];
-      if (i < 0) continue;
-      const uint4 a = *reinterpret_cast<const uint4*>(kg + i * sd.k_tok);
-      const uint4 b = *reinterpret_cast<const uint4*>(vg + i * sd.v_tok);
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        ka = fmaxf(ka, q8_finite_abs(q8_load(reinterpret_cast<const T*>(&a) + e)));
-        va = fmaxf(va, q8_finite_abs(q8_load(reinterpret_cast<const T*>(&b) + e)));
-      }
+  constexpr int PIECES = D / V;                    // of a row
+  __shared__ __attribute__((aligned(16))) int map[SEQ ? 1 : 1024];   // token of each place, -1: none
+  __shared__ uint32_t red[16];
+  __shared__ int leader;
+  extern __shared__ __attribute__((aligned(16))) uint8_t tile[];     // [D][part + 4]
+  const int t = threadIdx.x, nt = blockDim.x;
+  // Heads run fastest over the workgroups: a token's keys and values, often parts
+  // of one row, are then read at about the same time and over all memory
+  // channels (five fp32 prompts of 47662 tokens in rows of 4 KB, four heads: 69 us, with the
+  // blocks fastest 78).
+  const int wg = blockIdx.x / (2 * h_kv), hd = blockIdx.x - wg * 2 * h_kv;
+  const bool val = hd >= h_kv;                     // values, else keys
+  const int g = val ? hd - h_kv : hd;
+  int page, o0 = 0, o1 = B;                        // places that may be written
+  int i0 = 0;                                      // SEQ: token of place o0
+  if constexpr (SEQ) {
+    int s, c0, c1;
+    const long long j = seq_of_wg(wg, n_seqs, cu, B, N, &s, &c0, &c1);
+    if (c0 >= c1 || j < 0) return;
+    // token j B of the stretch, or its last, lies in block j if any does
+    const int begin = slots[c0], slot = slots[(int)min(c0 + j * B, (long long)c1 - 1)];
+    if (begin < 0 || slot < 0) return;
+    const long long row0 = c0 + j * B - begin % B;  // token of the block's first place
+    i0 = (int)max((long long)c0, row0);
+    const int i1 = (int)min((long long)c1, row0 + B);
+    if (i0 >= i1) return;
+    page = slot / B;
+    o0 = (int)(i0 - row0);
+    o1 = o0 + i1 - i0;
+  } else {
+    const int mine = t < N ? slots[t] : -1;        // beside the load of the workgroup's own
+    const int i = wg, slot = slots[i];
+    if (slot < 0) return;
+    page = slot / B;
+    const int base = page * B;
+    for (int o = t; o < B; o += nt) map[o] = -1;
+    if (t == 0) leader = 1;
+    __syncthreads();
+    for (int x = t; x < N; x += nt) {
+      const int o = (x == t ? mine : slots[x]) - base;
+      if ((unsigned)o >= (unsigned)B) continue;
+      if (x < i) leader = 0;
+      else atomicMax(&map[o], x);
     }
-  for (int off = 32; off > 0; off >>= 1) {
-    ka = fmaxf(ka, __shfl_xor(ka, off));
-    va = fmaxf(va, __shfl_xor(va, off));
+    __syncthreads();
+    if (!leader) return;
   }
-  if ((t & 63) == 0) {
-    red[0][t >> 6] = ka;
-    red[1][t >> 6] = va;
-  }
-  __syncthreads();
-  const long long at = (long long)page * h_kv + g;
-  const bool fresh = map[0] >= 0;
-  int e[2], grew[2];
+  if (page >= n_pages) return;
+
+  const int part = q8_part(B, D, sizeof(T));
+  const long long layer = blockIdx.z;
+  const long long at = (layer * n_pages + page) * h_kv + g;
+  uint8_t* scale = (val ? vs : ks) + at;
+  const int e_old = (int)*scale - 127;
+  const T* src = (val ? v + g * sd.v_head : k + g * sd.k_head) + layer * sd.layer;
+  const long long tok = val ? sd.v_tok : sd.k_tok;
+  auto token = [&](int o) {                        // token of a place, -1: none
+    if constexpr (SEQ) return o >= o0 && o < o1 ? i0 + o - o0 : -1;
+    else return map[o];
+  };
+  uint32_t raw[4][4];
+  // rows p0 + 4 (t / PIECES) .. of the part from place p0 on, piece t % PIECES
+  const int pc = t % PIECES, o = t / PIECES * 4;
+  auto load = [&](int p0) {
+    const int rows = min(part, B - p0);
 #pragma unroll
-  for (int x = 0; x < 2; ++x) {
-    const float m = fmaxf(fmaxf(red[x][0], red[x][1]), fmaxf(red[x][2], red[x][3]));
-    const int e_old = (int)(x ? vs : ks)[at] - 127;
-    const int e_new = q8_exponent(m);
-    e[x] = fresh ? e_new : max(e_new, e_old);
-    grew[x] = fresh ? 0 : e[x] - e_old;
-  }
-  __syncthreads();                                 // the old scales are read
-  if (t == 0) {
-    ks[at] = (uint8_t)(e[0] + 127);
-    vs[at] = (uint8_t)(e[1] + 127);
-  }
-  uint8_t* Kb = Kp + at * B * d;
-  uint8_t* Vb = Vp + at * B * d;
+    for (int q = 0; q < 4; ++q) {
+      const int r = o < rows ? token(p0 + o + q) : -1;
+      uint4 w = make_uint4(0, 0, 0, 0);
+      if (r >= 0) w = *reinterpret_cast<const uint4*>(src + r * tok + pc * V);
+      raw[q][0] = w.x;
+      raw[q][1] = w.y;
+      raw[q][2] = w.z;
+      raw[q][3] = w.w;
+    }
+  };
+  auto each = [&](auto&& f) {
 #pragma unroll
-  for (int x = 0; x < 2; ++x) {
-    if (grew[x] == 0) continue;
-    const float m = ldexpf(1.0f, -grew[x]);
-    uint4* c = reinterpret_cast<uint4*>(x ? Vb : Kb);
-    for (int i = t; i < B * d / 16; i += 256) {
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int y = 0; y < 4; ++y) f(raw[q][y]);
+  };
+  auto over_all = [&](uint32_t a) {                // the workgroup's largest
+    for (int off = 32; off > 0; off >>= 1) a = max(a, (uint32_t)__shfl_xor((int)a, off));
+    if ((t & 63) == 0) red[t >> 6] = a;
+    __syncthreads();
+    for (int w = 0; w < nt / 64; ++w) a = max(a, red[w]);
+    return a;
+  };
+  W m;
+  for (int p0 = 0; p0 < B; p0 += part) {
+    load(p0);
+    each([&](uint32_t w) { m.add(w); });
+  }
+  uint32_t top = over_all(m.largest());
+  const bool odd = top >= W::kInf;                 // infinity or NaN among them
+  if (odd) {
+    W f;
+    for (int p0 = 0; p0 < B; p0 += part) {
+      if (part < B) load(p0);
+      each([&](uint32_t& w) { f.add_finite(w); });
+    }
+    __syncthreads();                               // before red is written again
+    top = over_all(f.largest());
+  }
+  const bool fresh = token(0) >= 0;
+  const int e_new = q8_exponent(W::value(top));
+  const int e = fresh ? e_new : max(e_new, e_old);
+  if (t == 0) *scale = (uint8_t)(e + 127);
+  uint8_t* out = (val ? Vp : Kp) + at * B * D;
+  if (!fresh && e > e_old) {
+    const float f = ldexpf(1.0f, e_old - e);
+    uint4* c = reinterpret_cast<uint4*>(out);
+    for (int i = t; i < B * D / 16; i += nt) {
       uint4 w = c[i];
-      w.x = q8_rescale4(w.x, m);
-      w.y = q8_rescale4(w.y, m);
-      w.z = q8_rescale4(w.z, m);
-      w.w = q8_rescale4(w.w, m);
+      w.x = q8_rescale4(w.x, f);
+      w.y = q8_rescale4(w.y, f);
+      w.z = q8_rescale4(w.z, f);
+      w.w = q8_rescale4(w.w, f);
       c[i] = w;
     }
+    __syncthreads();                               // before the new codes go over them
   }
-  __syncthreads();                                 // before the new codes go over them
-  const float ki = ldexpf(1.0f, -e[0]), vi = ldexpf(1.0f, -e[1]);
-  for (int o0 = 0; o0 < B; o0 += kQ8Tile) {
-    const int oe = min(o0 + kQ8Tile, B);
-    if (row0 < per)
-      for (int o = o0 + row0; o < oe; o += per) {
-        const int i = map[o];
-        if (i < 0) continue;
-        const uint4 a = *reinterpret_cast<const uint4*>(kg + i * sd.k_tok);
-        const uint4 b = *reinterpret_cast<const uint4*>(vg + i * sd.v_tok);
-        const T* pa = reinterpret_cast<const T*>(&a);
-        const T* pb = reinterpret_cast<const T*>(&b);
-        uint32_t kw[V / 4];
+  const float sc = ldexpf(1.0f, e);
+  for (int p0 = 0; p0 < B; p0 += part) {
+    if (part < B) {
+      load(p0);
+      if (odd) {
+        W f;
+        each([&](uint32_t& w) { f.add_finite(w); });
+      }
+    }
+    const int rows = min(part, B - p0);
+    const int stride = part + 4;
+    if (o < rows && !val) {
 #pragma unroll
-        for (int x = 0; x < V; x += 4)
-          kw[x / 4] = q8_pack2(q8_load(pa + x), q8_load(pa + x + 1), ki) |
-                      q8_pack2(q8_load(pa + x + 2), q8_load(pa + x + 3), ki) << 16;
-        uint32_t* kd = reinterpret_cast<uint32_t*>(Kb + (long long)o * d + pc * V);
-#pragma unroll
-        for (int x = 0; x < V / 4; ++x) kd[x] = kw[x];
-#pragma unroll
-        for (int x = 0; x < V; x += 2) {
-          const uint32_t w = q8_pack2(q8_load(pb + x), q8_load(pb + x + 1), vi);
-          tile[(pc * V + x) * kQ8Stride + o - o0] = (uint8_t)w;
-          tile[(pc * V + x + 1) * kQ8Stride + o - o0] = (uint8_t)(w >> 8);
+      for (int q = 0; q < 4; ++q) {
+        if (token(p0 + o + q) < 0) continue;
+        const uint32_t (&w)[4] = raw[q];
+        uint8_t* dst = out + (long long)(p0 + o + q) * D + pc * V;
+        if constexpr (V == 8) {
+          const uint32_t lo = W::template codes<true>(W::template codes<false>(0, w[0], 0, sc), w[1], 0, sc);
+          const uint32_t hi = W::template codes<true>(W::template codes<false>(0, w[2], 0, sc), w[3], 0, sc);
+          *reinterpret_cast<uint2*>(dst) = make_uint2(lo, hi);
+        } else {
+          *reinterpret_cast<uint32_t*>(dst) =
+              W::template codes<true>(W::template codes<false>(0, w[0], w[1], sc), w[2], w[3], sc);
         }
       }
+    }
+    if (o < rows && val) {
+      // dims 2 y and 2 y + 1 of the four rows: bytes 0 and 1 of each half
+#pragma unroll
+      for (int y = 0; y < V / 2; ++y) {
+        auto two = [&](int q) { return V == 8 ? raw[q][y] : raw[q][2 * y % 4]; };
+        auto next = [&](int q) { return V == 8 ? 0u : raw[q][(2 * y + 1) % 4]; };
+        const uint32_t a = W::template codes<true>(W::template codes<false>(0, two(0), next(0), sc), two(1), next(1), sc);
+        const uint32_t b = W::template codes<true>(W::template codes<false>(0, two(2), next(2), sc), two(3), next(3), sc);
+        uint8_t* dst = tile + (pc * V + 2 * y) * stride + o;
+        *reinterpret_cast<uint32_t*>(dst) = __builtin_amdgcn_perm(b, a, 0x06040200u);
+        *reinterpret_cast<uint32_t*>(dst + stride) = __builtin_amdgcn_perm(b, a, 0x07050301u);
+      }
+    }
+    if (!val) continue;
     __syncthreads();
-    const int chunks = (oe - o0) / 16;             // B is a multiple of 16
-    for (int x = t; x < d * chunks; x += 256) {
-      const int dim = x / chunks, o = (x - dim * chunks) * 16;
-      uint32_t have = 0;
-      for (int q = 0; q < 16; ++q) have |= (uint32_t)(map[o0 + o + q] >= 0) << q;
-      const uint8_t* src = tile + dim * kQ8Stride + o;
-      uint8_t* dst = Vb + (long long)dim * B + o0 + o;
-      if (have == 0xffffu) {
-        const uint32_t* s4 = reinterpret_cast<const uint32_t*>(src);
+    const int chunks = rows / 16;
+    for (int x = t; x < D * chunks; x += nt) {
+      const int dim = x / chunks, c = (x - dim * chunks) * 16, p = p0 + c;
+      const uint32_t* s4 = reinterpret_cast<const uint32_t*>(tile + dim * stride + c);
+      uint8_t* dst = out + (long long)dim * B + p;
+      bool all = SEQ && p >= o0 && p + 16 <= o1;
+      if (!SEQ) {
+        all = true;
+        for (int q = 0; q < 16; ++q) all &= token(p + q) >= 0;
+      }
+      if (all) {
         *reinterpret_cast<uint4*>(dst) = make_uint4(s4[0], s4[1], s4[2], s4[3]);
-      } else if (have) {
+      } else {
         for (int q = 0; q < 16; ++q)
-          if (have >> q & 1) dst[q] = src[q];
+          if (token(p + q) >= 0) dst[q] = reinterpret_cast<const uint8_t*>(s4)[q];
       }
     }
     __syncthreads();
@@ -409,16 +600,27 @@ hipError_t launch_kv_append_q8(int dtype, int layers, const void* k, const void*
                                const int32_t* slots, int n_pages, int h_kv, int d, int B, void* Kp,
                                void* Vp, uint8_t* ks, uint8_t* vs, hipStream_t st) {
   const long long wgs = cu ? (long long)N / B + 2ll * n_seqs : N;
-  const dim3 grid((unsigned)wgs, (unsigned)h_kv, (unsigned)layers);
-  if (dtype == SW_BF16)
-    hipLaunchKernelGGL(kv_append_q8_kernel<uint16_t>, grid, dim3(256), 0, st,
-                       static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), sd, N, n_seqs,
-                       cu, slots, n_pages, h_kv, d, B, static_cast<uint8_t*>(Kp),
-                       static_cast<uint8_t*>(Vp), ks, vs);
-  else
-    hipLaunchKernelGGL(kv_append_q8_kernel<float>, grid, dim3(256), 0, st, static_cast<const float*>(k),
-                       static_cast<const float*>(v), sd, N, n_seqs, cu, slots, n_pages, h_kv, d, B,
-                       static_cast<uint8_t*>(Kp), static_cast<uint8_t*>(Vp), ks, vs);
+  const dim3 grid((unsigned)(wgs * 2 * h_kv), 1, (unsigned)layers);
+  uint8_t* kp = static_cast<uint8_t*>(Kp);
+  uint8_t* vp = static_cast<uint8_t*>(Vp);
+  // 64 bytes a thread, whole wavefronts
+  const int part = q8_part(B, d, dtype == SW_BF16 ? 2 : 4);
+  const int threads = (part * d * (dtype == SW_BF16 ? 2 : 4) / 64 + 63) / 64 * 64;
+#define SW_APPEND_(T, D, SEQ)                                                                      \
+  hipLaunchKernelGGL((kv_append_q8_kernel<T, D, SEQ>), grid, dim3((unsigned)threads),              \
+                     (unsigned)(D * (part + 4)), st, static_cast<const T*>(k),                     \
+                     static_cast<const T*>(v), sd, N, n_seqs, cu, slots, n_pages, h_kv, B, kp, vp, ks, vs)
+#define SW_APPEND(T)                                             \
+  do {                                                           \
+    if (d == 128) {                                              \
+      if (cu) SW_APPEND_(T, 128, true); else SW_APPEND_(T, 128, false); \
+    } else {                                                     \
+      if (cu) SW_APPEND_(T, 64, true); else SW_APPEND_(T, 64, false); \
+    }                                                            \
+  } while (0)
+  if (dtype == SW_BF16) SW_APPEND(uint16_t); else SW_APPEND(float);
+#undef SW_APPEND_
+#undef SW_APPEND
   return hipGetLastError();
 }
 
@@ -426,71 +628,140 @@ hipError_t launch_kv_append_q8(int dtype, int layers, const void* k, const void*
 // tokens out of the cache
 // ---------------------------------------------------------------------------
 
-// One workgroup per (block of a sequence's stretch, head): positions first[s]
-// .. first[s] + cu[s + 1] - cu[s] - 1 go to rows cu[s] .. of K, V [h_kv][N][d].
-// Values are exact in both types. A position without a page reads as zero.
-template <typename T>
+constexpr int kFetchTile = 64;                     // positions per workgroup, four chunks of 16
+constexpr int kFetchStride = kFetchTile + 4;       // bytes from one dimension's row to the next in LDS
+
+// One workgroup per (64 positions of a sequence, head): positions first[s] ..
+// first[s] + cu[s + 1] - cu[s] - 1 go to rows cu[s] .. of K, V [h_kv][N][d]. The
+// positions are taken in chunks of 16, each in its own block whatever the block
+// size. Values are exact in both types. A position without a page reads as zero.
+// All loads go out first; the values' 4 x 4 byte squares are transposed in
+// registers between LDS and the rows.
+template <typename T, int D>
 __global__ __launch_bounds__(256) void kv_fetch_q8_kernel(
     const uint8_t* __restrict__ Kp, const uint8_t* __restrict__ Vp, const uint8_t* __restrict__ ks,
-    const uint8_t* __restrict__ vs, int n_pages, int h_kv, int d, int B, int n_seqs, int b_max,
+    const uint8_t* __restrict__ vs, int n_pages, int h_kv, int B, int n_seqs, int b_max,
     const int32_t* __restrict__ tables, const int32_t* __restrict__ first,
     const int32_t* __restrict__ cu, int N, T* __restrict__ K, T* __restrict__ V) {
-  __shared__ __attribute__((aligned(16))) uint8_t tile[256 * kQ8Stride];
+  constexpr int E = 16 / (int)sizeof(T);           // values of a 16-byte store
+  constexpr int KP = D / E;                        // stores of a row
+  constexpr int NK = kFetchTile * KP / 256;        // keys' stores of a thread
+  constexpr int NV = D * 4 / 256;                  // its loads of 16 values' tokens
+  constexpr int NS = (KP * kFetchTile / 4 + 255) / 256;   // its blocks of E dims by four tokens
+  static_assert(NK * 256 == kFetchTile * KP && NV * 256 == D * 4, "whole pieces per thread");
+  __shared__ __attribute__((aligned(16))) uint8_t tile[D * kFetchStride];
+  __shared__ long long at4[4];
+  __shared__ int off4[4];
   const int t = threadIdx.x, g = blockIdx.y;
-  const int s = seq_of_wg(blockIdx.x, n_seqs, cu, B);
-  const int c0 = max(cu[s], 0), c1 = min(cu[s + 1], N);
-  if (c0 >= c1) return;
+  int s, c0, c1;
+  const long long u = seq_of_wg(blockIdx.x, n_seqs, cu, kFetchTile, N, &s, &c0, &c1);
+  if (c0 >= c1 || u < 0) return;
   const int p0 = first ? max(first[s], 0) : 0;
-  const long long j = blockIdx.x - (c0 / B + 2ll * s);
-  const long long blk = p0 / B + j;
-  // places lo .. hi - 1 of the block; place o is row row0 + o
-  const long long row0 = c0 + blk * B - p0;
-  const int lo = (int)max(0ll, c0 - row0), hi = (int)min((long long)B, c1 - row0);
+  const long long pt = (p0 / kFetchTile + u) * kFetchTile;   // the tile's first position
+  // places lo .. hi - 1 of the tile are asked for; place o is row row0 + o
+  const long long row0 = c0 + pt - p0;
+  const int lo = (int)max(0ll, c0 - row0), hi = (int)min((long long)kFetchTile, c1 - row0);
   if (lo >= hi) return;
-  const int page = blk < b_max ? tables[(long long)s * b_max + blk] : -1;
-  const bool have = (unsigned)page < (unsigned)n_pages;
-  const long long at = have ? (long long)page * h_kv + g : 0;
-  const float kf = q8_scale(ks[at]), vf = q8_scale(vs[at]);
-  const uint8_t* Kb = Kp + at * B * d;
-  const uint8_t* Vb = Vp + at * B * d;
-  T* Kd = K + ((long long)g * N + row0) * d;
-  T* Vd = V + ((long long)g * N + row0) * d;
-  auto put = [&](T* dst, uint32_t w, float f) {    // four values
-    const f32x2q a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false);
-    const f32x2q b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
-    if constexpr (sizeof(T) == 2)
-      *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(a[0] * f, a[1] * f), pack_bf16x2(b[0] * f, b[1] * f));
-    else
-      *reinterpret_cast<float4*>(dst) = make_float4(a[0] * f, a[1] * f, b[0] * f, b[1] * f);
-  };
-  const int words = d / 4;                         // of a row
-  for (int x = t; x < (hi - lo) * words; x += 256) {
-    const int o = lo + x / words, c = x % words;
-    const uint32_t w = have ? *reinterpret_cast<const uint32_t*>(Kb + (long long)o * d + 4 * c) : 0;
-    put(Kd + (long long)o * d + 4 * c, w, kf);
+  // page and head of each chunk (-1 without a page) and its place in the page
+  if (t < 4) {
+    const uint32_t p = (uint32_t)pt + 16 * t, j = p / (uint32_t)B;
+    const int page = j < (uint32_t)b_max && pt < (1ll << 31) ? tables[(long long)s * b_max + j] : -1;
+    at4[t] = (unsigned)page < (unsigned)n_pages ? (long long)page * h_kv + g : -1ll;
+    off4[t] = (int)(p - j * B);
   }
-  for (int o0 = lo / kQ8Tile * kQ8Tile; o0 < hi; o0 += kQ8Tile) {
-    const int chunks = (min(o0 + kQ8Tile, B) - o0) / 16;
-    for (int x = t; x < d * chunks; x += 256) {
-      const int dim = x / chunks, o = (x - dim * chunks) * 16;
-      const uint4 w = have ? *reinterpret_cast<const uint4*>(Vb + (long long)dim * B + o0 + o)
-                           : make_uint4(0, 0, 0, 0);
-      uint32_t* to = reinterpret_cast<uint32_t*>(tile + dim * kQ8Stride + o);
-      to[0] = w.x;
-      to[1] = w.y;
-      to[2] = w.z;
-      to[3] = w.w;
+  __syncthreads();
+  uint32_t kr[NK][E / 4];
+  float kf[NK];
+#pragma unroll
+  for (int i = 0; i < NK; ++i) {
+    const int x = t + 256 * i, o = x / KP, pc = x % KP;
+    const long long at = o >= lo && o < hi ? at4[o / 16] : -1;
+    kf[i] = 0.0f;
+    uint32_t w[2] = {0, 0};
+    if (at >= 0) {
+      const uint8_t* from = Kp + (at * B + off4[o / 16] + o % 16) * D + pc * E;
+      if constexpr (E == 8) {
+        const uint2 y = *reinterpret_cast<const uint2*>(from);
+        w[0] = y.x;
+        w[1] = y.y;
+      } else {
+        w[0] = *reinterpret_cast<const uint32_t*>(from);
+      }
+      kf[i] = q8_scale(ks[at]);
     }
-    __syncthreads();
-    const int a = max(lo, o0), b = min(hi, o0 + kQ8Tile);
-    for (int x = t; x < (b - a) * words; x += 256) {
-      const int o = a + x / words, c = x % words;
-      const uint8_t* from = tile + 4 * c * kQ8Stride + o - o0;
-      const uint32_t w = from[0] | (uint32_t)from[kQ8Stride] << 8 | (uint32_t)from[2 * kQ8Stride] << 16 |
-                         (uint32_t)from[3 * kQ8Stride] << 24;
-      put(Vd + (long long)o * d + 4 * c, w, vf);
+#pragma unroll
+    for (int e = 0; e < E / 4; ++e) kr[i][e] = w[e];
+  }
+  u32x4f vr[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int x = t + 256 * i, dim = x / 4, c = x % 4;
+    const long long at = 16 * c < hi && 16 * c + 16 > lo ? at4[c] : -1;
+    vr[i] = u32x4f{0, 0, 0, 0};
+    if (at >= 0) vr[i] = *reinterpret_cast<const u32x4f*>(Vp + (at * D + dim) * B + off4[c]);
+  }
+  // scales of the values that this thread writes out below: dims E dq .., tokens
+  // 4 (t / KP + 256 / KP i) ..
+  const int dq = t % KP;
+  float vf[NS];
+#pragma unroll
+  for (int i = 0; i < NS; ++i) {
+    const int o = (t / KP + 256 / KP * i) * 4;
+    const long long at = o < hi && o + 4 > lo ? at4[o / 16] : -1;
+    vf[i] = at >= 0 ? q8_scale(vs[at]) : 0.0f;
+  }
+  T* Kd = K + ((long long)g * N + row0) * D;
+  T* Vd = V + ((long long)g * N + row0) * D;
+  auto put = [&](T* dst, const uint32_t* w, float f) {   // E values
+    f32x2q a[E / 2];
+#pragma unroll
+    for (int e = 0; e < E / 4; ++e) {
+      a[2 * e] = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[e], false);
+      a[2 * e + 1] = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[e], true);
     }
-    __syncthreads();
+    if constexpr (E == 8)
+      *reinterpret_cast<uint4*>(dst) =
+          make_uint4(pack_bf16x2(a[0][0] * f, a[0][1] * f), pack_bf16x2(a[1][0] * f, a[1][1] * f),
+                     pack_bf16x2(a[2][0] * f, a[2][1] * f), pack_bf16x2(a[3][0] * f, a[3][1] * f));
+    else
+      *reinterpret_cast<float4*>(dst) = make_float4(a[0][0] * f, a[0][1] * f, a[1][0] * f, a[1][1] * f);
+  };
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int x = t + 256 * i, dim = x / 4, o = x % 4 * 16;
+    uint32_t* to = reinterpret_cast<uint32_t*>(tile + dim * kFetchStride + o);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) to[e] = vr[i][e];
+  }
+#pragma unroll
+  for (int i = 0; i < NK; ++i) {
+    const int x = t + 256 * i, o = x / KP, pc = x % KP;
+    if (o >= lo && o < hi) put(Kd + (long long)o * D + pc * E, kr[i], kf[i]);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < NS; ++i) {
+    const int o = (t / KP + 256 / KP * i) * 4;
+    if (o >= kFetchTile) break;
+    uint32_t w[4][E / 4];                          // four tokens' codes
+#pragma unroll
+    for (int e = 0; e < E / 4; ++e) {
+      uint32_t r[4];                               // dim E dq + 4 e + y, four tokens
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+        r[y] = *reinterpret_cast<const uint32_t*>(tile + (E * dq + 4 * e + y) * kFetchStride + o);
+      const uint32_t a0 = __builtin_amdgcn_perm(r[1], r[0], 0x05010400u);   // tokens 0 and 1 of dims 0, 1
+      const uint32_t a1 = __builtin_amdgcn_perm(r[1], r[0], 0x07030602u);   // tokens 2 and 3
+      const uint32_t b0 = __builtin_amdgcn_perm(r[3], r[2], 0x05010400u);
+      const uint32_t b1 = __builtin_amdgcn_perm(r[3], r[2], 0x07030602u);
+      w[0][e] = __builtin_amdgcn_perm(b0, a0, 0x05040100u);
+      w[1][e] = __builtin_amdgcn_perm(b0, a0, 0x07060302u);
+      w[2][e] = __builtin_amdgcn_perm(b1, a1, 0x05040100u);
+      w[3][e] = __builtin_amdgcn_perm(b1, a1, 0x07060302u);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (o + q >= lo && o + q < hi) put(Vd + (long long)(o + q) * D + E * dq, w[q], vf[i]);
   }
 }
 
@@ -498,17 +769,18 @@ hipError_t launch_kv_fetch_q8(int dtype, const void* Kp, const void* Vp, const u
                               const uint8_t* vs, int n_pages, int h_kv, int d, int B, int n_seqs,
                               int b_max, const int32_t* tables, const int32_t* first, const int32_t* cu,
                               int N, void* K, void* V, hipStream_t st) {
-  const dim3 grid((unsigned)(N / B + 2ll * n_seqs), (unsigned)h_kv);
+  const dim3 grid((unsigned)(N / kFetchTile + 2ll * n_seqs), (unsigned)h_kv);
   const uint8_t* kp = static_cast<const uint8_t*>(Kp);
   const uint8_t* vp = static_cast<const uint8_t*>(Vp);
-  if (dtype == SW_BF16)
-    hipLaunchKernelGGL(kv_fetch_q8_kernel<uint16_t>, grid, dim3(256), 0, st, kp, vp, ks, vs, n_pages,
-                       h_kv, d, B, n_seqs, b_max, tables, first, cu, N, static_cast<uint16_t*>(K),
-                       static_cast<uint16_t*>(V));
-  else
-    hipLaunchKernelGGL(kv_fetch_q8_kernel<float>, grid, dim3(256), 0, st, kp, vp, ks, vs, n_pages, h_kv,
-                       d, B, n_seqs, b_max, tables, first, cu, N, static_cast<float*>(K),
-                       static_cast<float*>(V));
+#define SW_FETCH(T, D)                                                                          \
+  hipLaunchKernelGGL((kv_fetch_q8_kernel<T, D>), grid, dim3(256), 0, st, kp, vp, ks, vs, n_pages, \
+                     h_kv, B, n_seqs, b_max, tables, first, cu, N, static_cast<T*>(K), static_cast<T*>(V))
+  if (dtype == SW_BF16) {
+    if (d == 128) SW_FETCH(uint16_t, 128); else SW_FETCH(uint16_t, 64);
+  } else {
+    if (d == 128) SW_FETCH(float, 128); else SW_FETCH(float, 64);
+  }
+#undef SW_FETCH
   return hipGetLastError();
 }
 

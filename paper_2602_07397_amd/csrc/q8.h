@@ -32,20 +32,6 @@ __device__ __forceinline__ int q8_exponent(float amax) {
   return max(e, -126);
 }
 
-// |x| where x is finite, else 0.
-__device__ __forceinline__ float q8_finite_abs(float x) {
-  const float a = fabsf(x);
-  return a < INFINITY ? a : 0.0f;                  // false for NaN
-}
-
-// Two codes of lo * inv and hi * inv (at most 448 in magnitude, or not finite:
-// those become NaN, which e4m3 has and infinity not) in the low 16 bits.
-__device__ __forceinline__ uint32_t q8_pack2(float lo, float hi, float inv) {
-  lo = fabsf(lo) < INFINITY ? lo * inv : __uint_as_float(0x7fc00000u);
-  hi = fabsf(hi) < INFINITY ? hi * inv : __uint_as_float(0x7fc00000u);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(lo, hi, 0, false) & 0xffffu;
-}
-
 // The four codes of a word, times m (a power of two of at most 1), rounded again.
 __device__ __forceinline__ uint32_t q8_rescale4(uint32_t w, float m) {
   const f32x2q a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false);

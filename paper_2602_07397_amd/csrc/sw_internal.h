@@ -154,10 +154,12 @@ struct DecodeQ8Steps {
   long long q, pool, idx, cnt, ws;
 };
 
+int64_t block_tables_workspace_bytes(int n_seqs, int64_t n_slots);
+
 hipError_t launch_block_tables(int n_seqs, int B, int b_max, const int32_t* old_len,
                                const int32_t* new_len, int32_t* tables, int32_t* free_pages,
                                int32_t* n_free, int n_pages, int rows, int n_slots, int32_t* slots,
-                               int32_t* cu, int32_t* pos, int32_t* status, hipStream_t st);
+                               int32_t* cu, int32_t* pos, int32_t* status, int32_t* ws, hipStream_t st);
 
 // cu NULL: every token by its slot alone.
 hipError_t launch_kv_append_q8(int dtype, int layers, const void* k, const void* v,

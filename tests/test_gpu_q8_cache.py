@@ -51,7 +51,7 @@ class _Requests:
 
 
 @pytest.mark.parametrize("n,B,rows", [(1, 64, 0), (5, 16, 0), (64, 64, 1), (63, 80, 3), (1030, 16, 0),
-                                      (2100, 128, 1)])
+                                      (2100, 128, 1), (2100, 16, 3), (1500, 64, 4)])
 def test_tables_over_many_calls(n, B, rows):
     b_max = 12
     r = _Requests(n, B, b_max, n * 8, seed=n + B)
@@ -66,12 +66,26 @@ def test_tables_over_many_calls(n, B, rows):
         r.check(new, rows, extra=7 * (step % 2))
 
 
-def test_tables_with_many_slots_take_the_second_launch():
+def test_tables_with_many_slots():
     r = _Requests(9, 64, 300, 2000, seed=4)
     r.check([0, 17000, 1, 64, 0, 63, 4000, 65, 128], extra=3)
     r.check([5, 17001, 0, 64, 9000, 64, 4000, 0, 129])
     p = _Requests(3, 16, 400, 1000, seed=5)          # padded rows, many of them
     p.check([5000, 0, 17], rows=5000)
+    p.check([1, 5000, 5000], rows=5000)
+    r.check([0] * 9, extra=9000)                     # everything back
+
+
+def test_tables_with_many_slots_that_cannot_be_served():
+    r = _Requests(2, 16, 1000, 600, seed=10)
+    r.check([100, 0])
+    state = (r.d_tables.clone(), r.d_free.clone(), r.d_n.clone())
+    for new, n_slots, status in (([9000, 1000], 9900, 1), ([9000, 100], 8000, 2)):
+        out = sw.block_tables(_i32(r.lens), _i32(new), 16, r.d_tables, r.d_free, r.d_n, n_slots)
+        assert int(out["status"]) == status and out["cu"].tolist() == [0, 0, 0] and out["pos"].tolist() == [99, -1]
+        assert torch.all(out["slots"] == -1)
+        for a, b in zip(state, (r.d_tables, r.d_free, r.d_n)):
+            assert torch.equal(a, b)
 
 
 def test_a_step_back_restores_tables_and_stack():

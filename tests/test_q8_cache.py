@@ -58,7 +58,7 @@ def _refused(fn, base, cases):
 
 
 def test_block_tables_refusals():
-    base = [3, 64, 10, FAKE, FAKE, FAKE, FAKE, FAKE, 30, 0, 100, FAKE, FAKE, FAKE, FAKE, None]
+    base = [3, 64, 10, FAKE, FAKE, FAKE, FAKE, FAKE, 30, 0, 100, FAKE, FAKE, FAKE, FAKE, None, 0, None]
     _refused("sw_block_tables", base, {
         "n_seqs": ({0: 0}, 1, "n_seqs"), "many": ({0: 65537}, 1, "n_seqs"), "B": ({1: 24}, 1, "B="),
         "B large": ({1: 1040}, 1, "B="), "b_max": ({2: 0}, 1, "b_max"), "b_max B": ({2: 1 << 25}, 1, "b_max"),
@@ -67,7 +67,10 @@ def test_block_tables_refusals():
         "slots large": ({10: 1 << 31}, 1, "n_slots"), "old": ({3: None}, 1, "old_len"),
         "new": ({4: None}, 1, "new_len"), "tables": ({5: FAKE + 2}, 1, "tables"), "free": ({6: None}, 1, "free"),
         "n_free": ({7: None}, 1, "n_free"), "slot list": ({11: None}, 1, "slots"),
-        "cu": ({12: None}, 1, "cu_seqlens"), "pos": ({13: None}, 1, "pos"), "status": ({14: None}, 1, "status")})
+        "cu": ({12: None}, 1, "cu_seqlens"), "pos": ({13: None}, 1, "pos"), "status": ({14: None}, 1, "status"),
+        "workspace": ({10: 100000}, 1, "workspace"), "small": ({10: 100000, 15: FAKE, 16: 32}, 1, "workspace_bytes")})
+    assert sw.load().sw_block_tables_workspace_bytes(0, 5) == -1
+    assert sw.load().sw_block_tables_workspace_bytes(3, 100) == 0
 
 
 def test_append_refusals():
@@ -76,7 +79,7 @@ def test_append_refusals():
     _refused("sw_kv_append_q8", base, {
         "dtype": ({0: 2}, 1, "dtype"), "k": ({1: FAKE + 8}, 1, "k is not"), "v": ({2: None}, 1, "v is NULL"),
         "stride": ({3: 100}, 1, "stride"), "negative": ({4: -1024}, 1, "stride"), "N": ({7: -1}, 1, "N="),
-        "many": ({7: 4097, 9: None}, 2, "4096"), "n_seqs": ({8: 0}, 1, "n_seqs"), "slots": ({10: None}, 1, "slots"),
+        "many": ({7: 4097, 9: None}, 2, "4096"), "launch": ({7: 1 << 30, 14: 16}, 2, "too many"), "n_seqs": ({8: 0}, 1, "n_seqs"), "slots": ({10: None}, 1, "slots"),
         "cu": ({9: FAKE + 1}, 1, "cu_seqlens"), "pages": ({11: 0}, 1, "n_pages"), "heads": ({12: 0}, 1, "h_kv"),
         "d": ({13: 96}, 2, "d=96"), "B": ({14: 8}, 1, "B="), "k pages": ({15: FAKE + 4}, 1, "k_pages"),
         "v pages": ({16: None}, 1, "v_pages"), "k scale": ({17: None}, 1, "k_scale"),
