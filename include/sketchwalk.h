@@ -484,7 +484,8 @@ int sw_kv_fetch_q8(int dtype, const void* k_pages, const void* v_pages, const ui
                    const int32_t* tables, const int32_t* first, const int32_t* cu_seqlens, int64_t N,
                    void* K, void* V, void* stream);
 
-/* Host-only: workspace bytes of sw_sparse_attn_decode_q8 (-1 on bad input). */
+/* Host-only: workspace bytes of sw_sparse_attn_decode_q8 (-1 on bad input; 0:
+   none, the workspace may be NULL). */
 int64_t sw_decode_attn_q8_workspace_bytes(int batch, int h_q, int h_kv, int d);
 
 /*
@@ -508,7 +509,7 @@ int sw_sparse_attn_decode_q8(int dtype, const void* q, const void* k_pages, cons
  * go to `slots` [batch] (as from sw_block_tables with rows = 1; negative: none),
  * the attention reads through tables [batch][b_max]. Pools are stacked over the
  * layers. workspace: >= sw_decode_attn_q8_workspace_bytes(...) bytes, 256-byte
- * aligned; with sw_decode_step_q8_workspace_bytes(...) several layers share an
+ * aligned (may be NULL when that is 0); with sw_decode_step_q8_workspace_bytes(...) several layers share an
  * attention launch. batch at most SW_MAX_APPEND_TOKENS. The sketch, the walk and
  * the selection are those of sw_decode_step, on the tokens as given; results are
  * bit-identical to the per-layer calls.

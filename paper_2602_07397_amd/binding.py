@@ -719,12 +719,13 @@ def sparse_attn_decode_q8(q: torch.Tensor, cache: dict, tables: torch.Tensor, po
         _shaped(O, (batch, h_q, d), "O")
     _shaped(idx, (batch, kmax), "idx")
     wsb = decode_attn_q8_workspace_bytes(batch, h_q, h_kv, d)
-    if workspace is None or workspace.numel() < wsb:
+    if wsb > 0 and (workspace is None or workspace.numel() < wsb):
         workspace = q.new_empty(wsb, dtype=_U8)
+    p_ws, wsb = (None, 0) if workspace is None else (_at(workspace, _U8, di, "workspace"), workspace.numel())
     _launch(di, load().sw_sparse_attn_decode_q8, _dtype_code(q), _at(q, dt, di, "q"), *pages, batch, h_q, h_kv,
             d, n_pages, _at(tables, _I32, di, "tables"), b_max, B, _vec(pos, batch, di, "pos"),
             _at(idx, _I32, di, "idx"), _vec(cnt, batch, di, "cnt"), kmax, float(scale), _at(O, dt, di, "O"),
-            _at(workspace, _U8, di, "workspace"), workspace.numel())
+            p_ws, wsb)
     return O
 
 
@@ -763,9 +764,10 @@ def decode_step_q8(q_new: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor
     for name, shape in shapes.items():
         _shaped(o[name], shape, name)
     least = decode_attn_q8_workspace_bytes(batch, h_q, h_kv, d)
-    if workspace is None or workspace.numel() < least:
+    if least > 0 and (workspace is None or workspace.numel() < least):
         wsb = int(load().sw_decode_step_q8_workspace_bytes(batch, h_q, h_kv, d))
         workspace = q_new.new_empty(wsb, dtype=_U8)
+    p_ws, wsb = (None, 0) if workspace is None else (_at(workspace, _U8, di, "workspace"), workspace.numel())
     dt = q_new.dtype
     _launch(di, load().sw_decode_step_q8, _dtype_code(q_new), L, batch, h_q, h_kv, d, r, n_pages, B, b_max,
             _at(q_new, dt, di, "q_new"), _at(k_new, dt, di, "k_new"), _at(v_new, dt, di, "v_new"), *pages,
@@ -773,5 +775,5 @@ def decode_step_q8(q_new: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor
             _vec(pos, batch, di, "pos"), _at(signs, torch.int8, di, "signs"), _at(cols, _I32, di, "cols"), s,
             walk_variant, k, density_pct, flags, kmax, float(scale), _at(o["rows"], torch.float64, di, "rows"),
             _at(o["idx"], _I32, di, "idx"), _at(o["cnt"], _I32, di, "cnt"), _at(o["O"], dt, di, "O"),
-            _at(workspace, _U8, di, "workspace"), workspace.numel())
+            p_ws, wsb)
     return o

@@ -27,9 +27,11 @@ HIPFLAGS = [
 # Per-source extras. The prefill attention kernel post-processes its score
 # MFMA results on the VALU and runs two wavefronts per SIMD within 256
 # registers each: the VGPR form of the MFMA instructions keeps accumulators in
-# VGPRs, so no AGPR-to-VGPR copies are needed.
+# VGPRs, so no AGPR-to-VGPR copies are needed. The 8-bit decode attention runs
+# three wavefronts per SIMD that way instead of two.
 EXTRA = {
     "attn_prefill.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "attn_decode_q8.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
 }
 
 

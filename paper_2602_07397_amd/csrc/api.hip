@@ -705,13 +705,24 @@ static int check_attn_q8(int batch, int h_q, int h_kv) {
   return SW_OK;
 }
 
+// Groups of 64 selected tokens of all heads are counted in 32 bits, chunks of 16
+// of a sequence too.
+static int check_selected(int batch, int h_kv, int kmax, int B) {
+  const int64_t chunks = (int64_t)kmax * (B / 16);
+  if (chunks >= (int64_t)1 << 31 || (chunks / 4 + 1) * batch * h_kv >= (int64_t)1 << 31)
+    return fail(SW_ERR_UNSUPPORTED, "kmax=%d blocks of %d tokens: too many for one call of %d sequences", kmax,
+                B, batch);
+  return SW_OK;
+}
+
 int64_t sw_decode_attn_q8_workspace_bytes(int batch, int h_q, int h_kv, int d) {
   if (check_attn_q8(batch, h_q, h_kv) != SW_OK) return -1;
   if (d != 64 && d != 128) {
     fail(SW_ERR_UNSUPPORTED, "8-bit cache head dim d=%d (64 or 128)", d);
     return -1;
   }
-  return sw_decode_attn_workspace_bytes(batch, h_q, h_kv, d);
+  ok();
+  return sw::attn_decode_q8_workspace_bytes(batch, h_q, h_kv, d);
 }
 
 int sw_sparse_attn_decode_q8(int dtype, const void* q, const void* k_pages, const void* v_pages,
@@ -726,6 +737,7 @@ int sw_sparse_attn_decode_q8(int dtype, const void* q, const void* k_pages, cons
   if (b_max < 1 || (int64_t)b_max * B >= (int64_t)1 << 31)
     return fail(SW_ERR_INVALID_ARG, "b_max=%d must be positive and b_max * B below 2^31", b_max);
   if (kmax < 1) return fail(SW_ERR_INVALID_ARG, "kmax=%d < 1", kmax);
+  CHECK(check_selected(batch, h_kv, kmax, B));
   CHECK(check_pages(k_pages, v_pages, k_scale, v_scale));
   CHECK(check_ptr(q, 16, "q"));
   CHECK(check_ptr(O, 16, "O"));
@@ -734,10 +746,12 @@ int sw_sparse_attn_decode_q8(int dtype, const void* q, const void* k_pages, cons
   CHECK(check_ptr(idx, 4, "idx"));
   CHECK(check_ptr(cnt, 4, "cnt"));
   const int64_t need = sw_decode_attn_q8_workspace_bytes(batch, h_q, h_kv, d);
-  CHECK(check_ptr(workspace, 256, "workspace"));
-  if (workspace_bytes < need)
-    return fail(SW_ERR_INVALID_ARG, "workspace_bytes=%lld < required %lld",
-                (long long)workspace_bytes, (long long)need);
+  if (need > 0) {
+    CHECK(check_ptr(workspace, 256, "workspace"));
+    if (workspace_bytes < need)
+      return fail(SW_ERR_INVALID_ARG, "workspace_bytes=%lld < required %lld",
+                  (long long)workspace_bytes, (long long)need);
+  }
   if (!(scale > 0.0f)) scale = 1.0f / sqrtf((float)d);
   hipError_t e = sw::launch_attn_decode_q8(dtype, 1, q, k_pages, v_pages, k_scale, v_scale, batch, h_q,
                                            h_kv, d, n_pages, tables, b_max, B, pos, idx, cnt, kmax, scale,
@@ -749,7 +763,7 @@ int sw_sparse_attn_decode_q8(int dtype, const void* q, const void* k_pages, cons
 // As sw_decode_step_workspace_bytes: eight layers in 64 MiB at most.
 int64_t sw_decode_step_q8_workspace_bytes(int batch, int h_q, int h_kv, int d) {
   const int64_t one = sw_decode_attn_q8_workspace_bytes(batch, h_q, h_kv, d);
-  if (one < 0) return one;
+  if (one <= 0) return one;
   int64_t n = ((int64_t)64 << 20) / one;
   n = n < 1 ? 1 : n > 8 ? 8 : n;
   return n * one;
@@ -778,6 +792,7 @@ int sw_decode_step_q8(int dtype, int layers, int batch, int h_q, int h_kv, int d
   CHECK(check_budget_args(k, density_pct, flags));
   const int need_k = last_row_budget(b_max, k, density_pct, flags);
   if (kmax < need_k) return fail(SW_ERR_INVALID_ARG, "kmax=%d < largest budget %d", kmax, need_k);
+  CHECK(check_selected(batch, h_kv, kmax, B));
   CHECK(check_ptr(q_new, 16, "q_new"));
   CHECK(check_ptr(k_new, 16, "k_new"));
   CHECK(check_ptr(v_new, 16, "v_new"));
@@ -793,10 +808,12 @@ int sw_decode_step_q8(int dtype, int layers, int batch, int h_q, int h_kv, int d
   CHECK(check_ptr(cnt, 4, "cnt"));
   CHECK(check_ptr(O, 16, "O"));
   const int64_t need = sw_decode_attn_q8_workspace_bytes(batch, h_q, h_kv, d);
-  CHECK(check_ptr(workspace, 256, "workspace"));
-  if (workspace_bytes < need)
-    return fail(SW_ERR_INVALID_ARG, "workspace_bytes=%lld < required %lld",
-                (long long)workspace_bytes, (long long)need);
+  if (need > 0) {
+    CHECK(check_ptr(workspace, 256, "workspace"));
+    if (workspace_bytes < need)
+      return fail(SW_ERR_INVALID_ARG, "workspace_bytes=%lld < required %lld",
+                  (long long)workspace_bytes, (long long)need);
+  }
   if (!(scale > 0.0f)) scale = 1.0f / sqrtf((float)d);
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   const int64_t kv_step = (int64_t)batch * h_kv * d;
@@ -812,7 +829,7 @@ int sw_decode_step_q8(int dtype, int layers, int batch, int h_q, int h_kv, int d
   const size_t esz = dtype == SW_BF16 ? 2 : 4;
   const int64_t q_step = (int64_t)batch * h_q * d * esz;
   const int64_t pool = (int64_t)n_pages * h_kv, page_step = pool * B * d;
-  const int64_t per = workspace_bytes / need;    // layers whose partials share a launch
+  const int64_t per = need > 0 ? workspace_bytes / need : layers;   // layers that share a launch
   for (int64_t l = 0; l < layers; l += per) {
     const int n = (int)(layers - l < per ? layers - l : per);
     e = sw::launch_attn_decode_q8(dtype, n, static_cast<const char*>(q_new) + l * q_step,

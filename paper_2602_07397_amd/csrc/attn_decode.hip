@@ -561,9 +561,7 @@ __global__ __launch_bounds__(256, 2) void attn_decode_f32_kernel(
 // four sums are added in order. The splits' outputs come from another launch, so the kernel is two
 // dependent loads and one barrier long: 32 splits took 10.5 us as a loop over
 // the splits (batch 1, 32 heads).
-// NANS: a sum of weights that is not a number gives such an output (the 8-bit
-// cache's attention); without, it gives 0.
-template <typename T, int D, bool NANS, int NLOAD>
+template <typename T, int D, int NLOAD>
 __global__ __launch_bounds__(256) void attn_merge_kernel(const float* __restrict__ ws, int S,
                                                          long long n_hu, T* __restrict__ O,
                                                          long long ws_step, float ms) {
@@ -601,7 +599,7 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(const float* __restrict
   if (threadIdx.x >= D) return;
   const int dim = threadIdx.x;
   const float sum = ((part[0][dim] + part[1][dim]) + part[2][dim]) + part[3][dim];
-  const float v = (NANS ? Lsum != 0.0f : Lsum > 0.0f) ? sum / Lsum : 0.0f;
+  const float v = Lsum > 0.0f ? sum / Lsum : 0.0f;
   const long long at = (blockIdx.y * n_hu + hu) * D + dim;
   if constexpr (sizeof(T) == 2)
     reinterpret_cast<uint16_t*>(O)[at] = f32_to_bf16(v);
@@ -612,7 +610,7 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(const float* __restrict
 // One split: a wavefront per (sequence, query head). A call at batch 64, 2000
 // tokens, 32 heads over 8 of d = 128: 26.8 us with the four of the kernel above,
 // 25.2 with one (fp32 45.1 and 43.8).
-template <typename T, int D, bool NANS>
+template <typename T, int D>
 __global__ __launch_bounds__(256) void attn_merge_one_kernel(const float* __restrict__ ws,
                                                              long long n_hu, T* __restrict__ O,
                                                              long long ws_step) {
@@ -629,7 +627,7 @@ __global__ __launch_bounds__(256) void attn_merge_one_kernel(const float* __rest
   const long long at = (blockIdx.y * n_hu + hu) * D + l * V;
 #pragma unroll
   for (int e = 0; e < V; ++e) {
-    const float v = (NANS ? Lsum != 0.0f : Lsum > 0.0f) ? o[e] / Lsum : 0.0f;
+    const float v = Lsum > 0.0f ? o[e] / Lsum : 0.0f;
     if constexpr (sizeof(T) == 2)
       reinterpret_cast<uint16_t*>(O)[at + e] = f32_to_bf16(v);
     else
@@ -679,46 +677,6 @@ hipError_t noalloc_scratch(void** out) {
   return hipSuccess;
 }
 
-namespace {
-
-template <typename T, int D, bool NANS>
-void launch_merge_t(int layers, long long n_hu, int S, const float* ws, void* O, float ms,
-                    hipStream_t st) {
-  const long long ws_step = n_hu * S * (D + 2);
-  const dim3 mgrid((unsigned)n_hu, (unsigned)layers);
-  T* o = reinterpret_cast<T*>(O);
-#define SW_MERGE_N(N)                                                                             \
-  hipLaunchKernelGGL((attn_merge_kernel<T, D, NANS, N>), mgrid, dim3(256), 0, st, ws, S, n_hu, o, \
-                     ws_step, ms)
-  if (S == 1)
-    hipLaunchKernelGGL((attn_merge_one_kernel<T, D, NANS>), dim3((mgrid.x + 3) / 4, mgrid.y), dim3(256),
-                       0, st, ws, n_hu, o, ws_step);
-  else if (S <= 4) SW_MERGE_N(1);
-  else if (S <= 16) SW_MERGE_N(4);
-  else SW_MERGE_N(kDecodeMaxSplits / 4);
-#undef SW_MERGE_N
-}
-
-template <bool NANS>
-void launch_merge(int dtype, int layers, long long n_hu, int d, int S, const float* ws, void* O,
-                  float ms, hipStream_t st) {
-  if (dtype == SW_BF16) {
-    if (d == 128) launch_merge_t<uint16_t, 128, NANS>(layers, n_hu, S, ws, O, ms, st);
-    else launch_merge_t<uint16_t, 64, NANS>(layers, n_hu, S, ws, O, ms, st);
-  } else {
-    if (d == 128) launch_merge_t<float, 128, NANS>(layers, n_hu, S, ws, O, ms, st);
-    else launch_merge_t<float, 64, NANS>(layers, n_hu, S, ws, O, ms, st);
-  }
-}
-
-}  // namespace
-
-hipError_t launch_attn_merge_q8(int dtype, int layers, int batch, int h_q, int d, int S,
-                                const float* ws, void* O, hipStream_t st) {
-  launch_merge<true>(dtype, layers, (long long)batch * h_q, d, S, ws, O, 1.0f, st);
-  return hipGetLastError();
-}
-
 hipError_t launch_attn_decode(int dtype, int layers, const void* q, const void* Kc, const void* Vc,
                               int batch, int h_q, int h_kv, int d, int T_max, int B,
                               const int32_t* pos, const int32_t* idx, const int32_t* cnt, int kmax,
@@ -728,34 +686,54 @@ hipError_t launch_attn_decode(int dtype, int layers, const void* q, const void* 
   const dim3 grid((unsigned)(batch * h_kv * S), (unsigned)layers);
   const float sl2 = scale * kLog2eD;
   const long long n_hu = (long long)batch * h_q;
+  const dim3 mgrid((unsigned)n_hu, (unsigned)layers);
   DecodeAttnSteps ls;
   ls.q = n_hu * d;
   ls.cache = (long long)batch * h_kv * T_max * d;
   ls.idx = (long long)batch * kmax;
   ls.cnt = batch;
   ls.ws = n_hu * S * (d + 2);
+#define SW_MERGE_N(T, D, N)                                                                    \
+  hipLaunchKernelGGL((attn_merge_kernel<T, D, N>), mgrid, dim3(256), 0, st, ws, S, n_hu,       \
+                     reinterpret_cast<T*>(O), ls.ws, sizeof(T) == 4 ? sl2 : 1.0f)
+#define SW_MERGE(T, D)                                      \
+  do {                                                      \
+    if (S == 1)                                             \
+      hipLaunchKernelGGL((attn_merge_one_kernel<T, D>), dim3((mgrid.x + 3) / 4, mgrid.y), dim3(256), 0, \
+                         st, ws, n_hu, reinterpret_cast<T*>(O), ls.ws); \
+    else if (S <= 4) SW_MERGE_N(T, D, 1);                   \
+    else if (S <= 16) SW_MERGE_N(T, D, 4);                  \
+    else SW_MERGE_N(T, D, kDecodeMaxSplits / 4);            \
+  } while (0)
   if (dtype == SW_BF16) {
     auto qq = reinterpret_cast<const uint16_t*>(q);
     auto kk = reinterpret_cast<const uint16_t*>(Kc);
     auto vv = reinterpret_cast<const uint16_t*>(Vc);
-    if (d == 128)
+    if (d == 128) {
       hipLaunchKernelGGL(attn_decode_mfma_kernel<128>, grid, dim3(256), 0, st, qq, kk, vv, h_kv, G,
                          T_max, B, pos, idx, cnt, kmax, sl2, S, ws, ls);
-    else
+      SW_MERGE(uint16_t, 128);
+    } else {
       hipLaunchKernelGGL(attn_decode_mfma_kernel<64>, grid, dim3(256), 0, st, qq, kk, vv, h_kv, G,
                          T_max, B, pos, idx, cnt, kmax, sl2, S, ws, ls);
+      SW_MERGE(uint16_t, 64);
+    }
   } else {
     auto qq = reinterpret_cast<const float*>(q);
     auto kk = reinterpret_cast<const float*>(Kc);
     auto vv = reinterpret_cast<const float*>(Vc);
-    if (d == 128)
+    if (d == 128) {
       hipLaunchKernelGGL(attn_decode_f32_kernel<128>, grid, dim3(256), 0, st, qq, kk, vv, h_kv, G,
                          T_max, B, pos, idx, cnt, kmax, sl2, S, ws, ls);
-    else
+      SW_MERGE(float, 128);
+    } else {
       hipLaunchKernelGGL(attn_decode_f32_kernel<64>, grid, dim3(256), 0, st, qq, kk, vv, h_kv, G,
                          T_max, B, pos, idx, cnt, kmax, sl2, S, ws, ls);
+      SW_MERGE(float, 64);
+    }
   }
-  launch_merge<false>(dtype, layers, n_hu, d, S, ws, O, dtype == SW_BF16 ? 1.0f : sl2, st);
+#undef SW_MERGE
+#undef SW_MERGE_N
   return hipGetLastError();
 }
 

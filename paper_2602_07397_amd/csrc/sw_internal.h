@@ -134,11 +134,6 @@ hipError_t launch_attn_decode(int dtype, int layers, const void* q, const void* 
                               const int32_t* pos, const int32_t* idx, const int32_t* cnt, int kmax,
                               float scale, void* O, float* ws, hipStream_t st);
 
-// The merge of the 8-bit cache's split-K partials of `layers` layers
-// (attn_decode.hip), maxima in log2 units.
-hipError_t launch_attn_merge_q8(int dtype, int layers, int batch, int h_q, int d, int S,
-                                const float* ws, void* O, hipStream_t st);
-
 // ---------------------------------------------------------------------------
 // paged 8-bit cache
 // ---------------------------------------------------------------------------
@@ -172,7 +167,9 @@ hipError_t launch_kv_fetch_q8(int dtype, const void* Kp, const void* Vp, const u
                               int b_max, const int32_t* tables, const int32_t* first, const int32_t* cu,
                               int N, void* K, void* V, hipStream_t st);
 
-// ws: decode_attn_splits(batch, h_kv) partials per (sequence, query head) and layer.
+// Per layer; 0 for batches whose (sequence, KV head) pairs have a workgroup each.
+int64_t attn_decode_q8_workspace_bytes(int batch, int h_q, int h_kv, int d);
+
 hipError_t launch_attn_decode_q8(int dtype, int layers, const void* q, const void* Kp, const void* Vp,
                                  const uint8_t* ks, const uint8_t* vs, int batch, int h_q, int h_kv,
                                  int d, int n_pages, const int32_t* tables, int b_max, int B,
