@@ -2,6 +2,7 @@
 // as e4m3 codes): softmax attention of one token per sequence over the tokens
 // of the selected key blocks, split-K over those tokens.
 #include <climits>
+#include <type_traits>
 
 #include "q8.h"
 #include "sw_common.h"
@@ -415,19 +416,39 @@ __global__ __launch_bounds__(256) void attn_decode_q8_kernel(
   }
 }
 
+// A value with that of the lane 1, 2, 4 and 8 further in its row of 16 lanes.
+template <int BY>
+__device__ __forceinline__ float q8_ror(float v) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x120 + BY, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float q8_wave_max(float v) {
+  v = fmaxf(v, q8_ror<1>(v));
+  v = fmaxf(v, q8_ror<2>(v));
+  v = fmaxf(v, q8_ror<4>(v));
+  return q8_xmax(fmaxf(v, q8_ror<8>(v)));
+}
+__device__ __forceinline__ float q8_wave_sum(float v) {
+  v += q8_ror<1>(v);
+  v += q8_ror<2>(v);
+  v += q8_ror<4>(v);
+  return q8_xsum(v + q8_ror<8>(v));
+}
+
 // Merge of the partial sums of one (sequence, query head): those of the
-// workgroups that shared its groups. Lane s of every wavefront holds the s-th
-// one's maximum and sum; wavefront w adds the outputs of w, w + 4, ...
+// workgroups that shared its groups, at most 64. Lane s of every wavefront holds
+// the s-th one's maximum and sum; wavefront w adds the outputs of w, w + 4, ...,
+// all on their way before the first is needed: two dependent loads, one barrier.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void attn_merge_q8_kernel(const float* __restrict__ ws, int batch, int h_kv,
                                                             int G, T* __restrict__ O, DecodeQ8Steps ls) {
+  static_assert(kQ8Splits <= 64, "one partial sum per lane");
   constexpr int V = D / 64;                        // output dims per lane
   typedef float vec __attribute__((ext_vector_type(V)));
   __shared__ float part[4][D];
   const long long layer = blockIdx.y;
   ws += layer * ls.ws;
   O += layer * ls.q;
-  const int t = threadIdx.x, w = t >> 6, l = t & 63;
+  const int t = threadIdx.x, w = __builtin_amdgcn_readfirstlane(t >> 6), l = t & 63;
   const int pair = blockIdx.x / G, u = blockIdx.x - pair * G;
   const int2 info = reinterpret_cast<const int2*>(ws)[pair];
   const int S = info.y;
@@ -438,21 +459,28 @@ __global__ __launch_bounds__(256) void attn_merge_q8_kernel(const float* __restr
   }
   if (S == 1) return;                              // its workgroup wrote the output
   const long long pairs = (long long)batch * h_kv, seg = info.x;
-  const float* ml = ws + q8_ws_sums(pairs) + (seg * G + u) * 2;
-  const float* o = ws + q8_ws_outs(pairs, G) + (seg * G + u) * D;
-  float M = -INFINITY;
-  for (int s = l; s < S; s += 64) M = fmaxf(M, ml[(long long)s * G * 2]);
-  for (int off = 32; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
-  float Lsum = 0.0f;
+  const float2 ml = *reinterpret_cast<const float2*>(ws + q8_ws_sums(pairs) + ((seg + min(l, S - 1)) * G + u) * 2);
+  const float* o = ws + q8_ws_outs(pairs, G) + (seg * G + u) * D + l * V;
   vec acc = {};
-  if (M != -INFINITY) {
-    for (int s = l; s < S; s += 64)
-      Lsum += ml[(long long)s * G * 2 + 1] * q8_exp2(ml[(long long)s * G * 2] - M);
-    for (int off = 32; off > 0; off >>= 1) Lsum += __shfl_xor(Lsum, off);
-#pragma unroll 8
-    for (int s = w; s < S; s += 4)
-      acc += *reinterpret_cast<const vec*>(o + (long long)s * G * D + l * V) * q8_exp2(ml[(long long)s * G * 2] - M);
-  }
+  float Lsum;
+  auto add = [&](auto n) {
+    constexpr int N = decltype(n)::value;
+    vec x[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = *reinterpret_cast<const vec*>(o + (long long)min(w + 4 * i, S - 1) * G * D);
+    const float m = l < S ? ml.x : -INFINITY;
+    const float M = q8_wave_max(m);
+    // without any token all weigh 0
+    const float sc = M != -INFINITY && l < S ? q8_exp2(m - M) : 0.0f;
+    Lsum = q8_wave_sum(l < S ? ml.y * sc : 0.0f);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int s = w + 4 * i;
+      if (s < S) acc += x[i] * __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sc), s));
+    }
+  };
+  if (S <= 16) add(std::integral_constant<int, 4>());
+  else add(std::integral_constant<int, 16>());
 #pragma unroll
   for (int e = 0; e < V; ++e) part[w][l * V + e] = acc[e];
   __syncthreads();
