@@ -137,8 +137,11 @@ __device__ __forceinline__ void q8_store(T* O, long long at, float v) {
 
 // Workgroup of four wavefronts over a part of a (sequence, head)'s groups of 64
 // selected tokens, four chunks of 16, whichever blocks they are in; each wavefront
-// takes a quarter. A lane holds the page and place of one chunk of 16 groups
-// ahead, so that the loop has neither barriers nor index loads.
+// takes every fourth group, so that the wavefronts together read 256 tokens of a
+// value row at about the same time (a block of 128 has a 128-byte line of it in
+// two groups; quarters of the range one after the other take 112 us where this takes
+// 96). A lane holds the page and place of one chunk of 16 groups ahead,
+// so that the loop has neither barriers nor index loads.
 //   S = K q^T      v_mfma_f32_16x16x32_bf16: row m of the x-th product is token
 //                  4 x + m % 4 of chunk m / 4, so lane (n, lg) receives 16
 //                  tokens of head n, all of chunk lg: its scale, its first token
@@ -210,10 +213,6 @@ __global__ __launch_bounds__(256) void attn_decode_q8_kernel(
   }
   const int p = part.p, bc = p / B;
   const int nch = max(0, min(part.have, kmax)) * cpb;   // chunks of the sequence
-  // this wavefront's quarter
-  const int wa = ga + w * ((gb - ga) >> 2) + min(w, (gb - ga) & 3);
-  const int wb = wa + ((gb - ga) >> 2) + (w < ((gb - ga) & 3));
-
   bf16x8q qf[NP][NK][2];
   {
     const bool hv = ln < G;
@@ -248,7 +247,11 @@ __global__ __launch_bounds__(256) void attn_decode_q8_kernel(
   // the lane's chunk of the listed groups: page, first token (INT_MAX: none of it
   // counts), place in the page
   int c_page = 0, c_t0 = INT_MAX, c_off = 0;
-  // The loads of a group. Its scales are loaded beside its codes.
+  // The loads of a group. Its scales are loaded beside its codes. Keys are read
+  // once, whole lines at a time, and loaded as a stream; of the values, larger
+  // blocks leave part of a line to another group (16 sequences of 65536 tokens:
+  // all loads as a stream 80 us at blocks of 64, 96 at 128, 114 at 1024; the
+  // values' without 78, 92, 102).
   struct Group {
     u32x4q k[4][NK], v[NT];
     uint32_t ks, vs;
@@ -271,7 +274,7 @@ __global__ __launch_bounds__(256) void attn_decode_q8_kernel(
     r.vs = vs[at_v];
 #pragma unroll
     for (int t = 0; t < NT; ++t)
-      r.v[t] = __builtin_nontemporal_load(reinterpret_cast<const u32x4q*>(vp + t * 16 * B));
+      r.v[t] = *reinterpret_cast<const u32x4q*>(vp + t * 16 * B);
     // all of them are out before the first is waited for (the scheduler
     // otherwise moves the values' loads behind the scores)
     __builtin_amdgcn_sched_barrier(0);
@@ -345,11 +348,11 @@ __global__ __launch_bounds__(256) void attn_decode_q8_kernel(
       }
     }
   };
-  for (int g0 = wa; g0 < wb; g0 += 16) {
+  for (int g0 = ga + w; g0 < gb; g0 += 64) {
     c_page = c_off = 0;
     c_t0 = INT_MAX;
-    const int ch = g0 * 4 + l;
-    if (ch < min(nch, wb * 4)) {
+    const int gl = g0 + (l & ~3), ch = gl * 4 + (l & 3);
+    if (gl < gb && ch < nch) {
       const int e = ch / cpb, off = (ch - e * cpb) * 16;
       const int j = idx[(long long)bi * kmax + e];
       if (j >= 0 && j <= bc && j * B + off <= p) {
@@ -361,7 +364,7 @@ __global__ __launch_bounds__(256) void attn_decode_q8_kernel(
         }
       }
     }
-    for (int i = 0; i < 16 && g0 + i < wb; ++i) {
+    for (int i = 0; i < 16 && g0 + 4 * i < gb; ++i) {
       Group r;
       issue(i, r);
       compute(r);
