@@ -153,8 +153,8 @@ __device__ __forceinline__ void q8_store(T* O, long long at, float v) {
 // fp32: q and the weights go in as sums of three bf16 numbers (24 bits).
 // SHARE: the groups are shared out as Q8Plan does; a (sequence, head) of one
 // workgroup is written out by it, others leave partial sums. Otherwise a
-// workgroup per (sequence, head).
-template <typename T, int D, bool SHARE>
+// workgroup per (sequence, head). STREAM: the values' loads, see below.
+template <typename T, int D, bool SHARE, bool STREAM>
 __global__ __launch_bounds__(256) void attn_decode_q8_kernel(
     const T* __restrict__ q, const uint8_t* __restrict__ Kp, const uint8_t* __restrict__ Vp,
     const uint8_t* __restrict__ ks, const uint8_t* __restrict__ vs, int batch, int h_kv, int G, int n_pages,
@@ -247,11 +247,11 @@ __global__ __launch_bounds__(256) void attn_decode_q8_kernel(
   // the lane's chunk of the listed groups: page, first token (INT_MAX: none of it
   // counts), place in the page
   int c_page = 0, c_t0 = INT_MAX, c_off = 0;
-  // The loads of a group. Its scales are loaded beside its codes. Keys are read
-  // once, whole lines at a time, and loaded as a stream; of the values, larger
-  // blocks leave part of a line to another group (16 sequences of 65536 tokens:
-  // all loads as a stream 80 us at blocks of 64, 96 at 128, 114 at 1024; the
-  // values' without 78, 92, 102).
+  // The loads of a group. Its scales are loaded beside its codes. Whole
+  // lines that are read once are loaded as a stream; of the values, blocks over 64
+  // leave part of a line to another group (16 sequences of 65536 tokens, values as
+  // a stream and not: 69.1 and 71.9 us at blocks of 64, 96 and 92 at 128, 114 and
+  // 102 at 1024).
   struct Group {
     u32x4q k[4][NK], v[NT];
     uint32_t ks, vs;
@@ -273,8 +273,11 @@ __global__ __launch_bounds__(256) void attn_decode_q8_kernel(
     r.ks = ks[at_v];
     r.vs = vs[at_v];
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
-      r.v[t] = *reinterpret_cast<const u32x4q*>(vp + t * 16 * B);
+    for (int t = 0; t < NT; ++t) {
+      const u32x4q* from = reinterpret_cast<const u32x4q*>(vp + t * 16 * B);
+      if constexpr (STREAM) r.v[t] = __builtin_nontemporal_load(from);
+      else r.v[t] = *from;
+    }
     // all of them are out before the first is waited for (the scheduler
     // otherwise moves the values' loads behind the scores)
     __builtin_amdgcn_sched_barrier(0);
@@ -516,18 +519,18 @@ hipError_t launch_attn_decode_q8(int dtype, int layers, const void* q, const voi
   const dim3 mgrid((unsigned)(batch * h_q), (unsigned)layers);
   const uint8_t* kp = static_cast<const uint8_t*>(Kp);
   const uint8_t* vp = static_cast<const uint8_t*>(Vp);
-#define SW_Q8_(T, D, SHARE)                                                                           \
-  hipLaunchKernelGGL((attn_decode_q8_kernel<T, D, SHARE>), grid, dim3(256), 0, st,                    \
+#define SW_Q8_(T, D, SHARE, STREAM)                                                                   \
+  hipLaunchKernelGGL((attn_decode_q8_kernel<T, D, SHARE, STREAM>), grid, dim3(256), 0, st,            \
                      static_cast<const T*>(q), kp, vp, ks, vs, batch, h_kv, G, n_pages, tables, b_max, \
                      B, pos, idx, cnt, kmax, sl2, static_cast<T*>(O), ws, ls)
 #define SW_Q8(T, D)                                                                                 \
   do {                                                                                              \
     if (share) {                                                                                    \
-      SW_Q8_(T, D, true);                                                                           \
+      if (B <= 64) SW_Q8_(T, D, true, true); else SW_Q8_(T, D, true, false);                        \
       hipLaunchKernelGGL((attn_merge_q8_kernel<T, D>), mgrid, dim3(256), 0, st, ws, batch, h_kv, G, \
                          static_cast<T*>(O), ls);                                                   \
     } else {                                                                                        \
-      SW_Q8_(T, D, false);                                                                          \
+      if (B <= 64) SW_Q8_(T, D, false, true); else SW_Q8_(T, D, false, false);                      \
     }                                                                                               \
   } while (0)
   if (dtype == SW_BF16) {
