@@ -719,12 +719,17 @@ __global__ __launch_bounds__(256) void kv_fetch_q8_kernel(
       a[2 * e] = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[e], false);
       a[2 * e + 1] = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[e], true);
     }
-    if constexpr (E == 8)
-      *reinterpret_cast<uint4*>(dst) =
-          make_uint4(pack_bf16x2(a[0][0] * f, a[0][1] * f), pack_bf16x2(a[1][0] * f, a[1][1] * f),
-                     pack_bf16x2(a[2][0] * f, a[2][1] * f), pack_bf16x2(a[3][0] * f, a[3][1] * f));
-    else
-      *reinterpret_cast<float4*>(dst) = make_float4(a[0][0] * f, a[0][1] * f, a[1][0] * f, a[1][1] * f);
+    // as a stream: written over the caches they would put out what is still to be
+    // read (32768 tokens to bf16 44 -> 31 us, the pages then partly cached)
+    u32x4f out;
+    if constexpr (E == 8) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) out[e] = pack_bf16x2(a[e][0] * f, a[e][1] * f);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) out[e] = __float_as_uint(a[e / 2][e % 2] * f);
+    }
+    __builtin_nontemporal_store(out, reinterpret_cast<u32x4f*>(dst));
   };
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
