@@ -9,6 +9,7 @@ built or cannot be loaded, every call raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional, Sequence, Tuple
 
@@ -602,17 +603,23 @@ def _launch(di: int, fn, *args) -> None:
 def _pool(cache: dict, layers: Optional[int] = None):
     """(device index, n_pages, h_kv, B, d, pointers) of a cache as new_cache_q8 makes it."""
     k, v, ks, vs = cache["k"], cache["v"], cache["k_scale"], cache["v_scale"]
-    lead = () if layers is None else (layers,)
     shape = k.shape
-    if len(shape) != 4 + len(lead) or shape[:-4] != lead:
-        raise SketchWalkError(f"cache k of shape {tuple(shape)}: {lead + ('n_pages', 'h_kv', 'B', 'd')} needed")
-    n_pages, h_kv, B, d = shape[-4:] if lead else shape
-    if v.shape != (*lead, n_pages, h_kv, d, B):
-        raise SketchWalkError(f"cache v of shape {tuple(v.shape)} beside k of shape {tuple(shape)}")
-    heads = (*lead, n_pages, h_kv)
-    if ks.shape != heads or vs.shape != heads:
-        raise SketchWalkError(f"cache k_scale, v_scale of shapes {tuple(ks.shape)}, {tuple(vs.shape)}: {heads} needed")
-    di = _gpu(k, "cache k")
+    di = k.get_device()
+    if layers is None:
+        fits = len(shape) == 4 and v.shape == (shape[0], shape[1], shape[3], shape[2]) \
+            and ks.shape == shape[:2] and vs.shape == ks.shape
+    else:
+        fits = len(shape) == 5 and shape[0] == layers and v.shape == (*shape[:3], shape[4], shape[3]) \
+            and ks.shape == shape[:3] and vs.shape == ks.shape
+    if not fits:
+        lead = "" if layers is None else f"{layers}, "
+        raise SketchWalkError(
+            f"cache of shapes k {tuple(shape)}, v {tuple(v.shape)}, k_scale {tuple(ks.shape)}, v_scale "
+            f"{tuple(vs.shape)}: ({lead}n_pages, h_kv, B, d), ({lead}n_pages, h_kv, d, B) and twice "
+            f"({lead}n_pages, h_kv) needed")
+    if di < 0:
+        raise SketchWalkError("cache k must be a CUDA (HIP) tensor")
+    n_pages, h_kv, B, d = shape[-4:]
     return di, n_pages, h_kv, B, d, (_at(k, E4M3, di, "cache k"), _at(v, E4M3, di, "cache v"),
                                      _at(ks, _U8, di, "cache k_scale"), _at(vs, _U8, di, "cache v_scale"))
 
@@ -692,6 +699,7 @@ def kv_fetch_q8(cache: dict, tables: torch.Tensor, first: Optional[torch.Tensor]
     return K, V
 
 
+@functools.lru_cache(maxsize=None)
 def decode_attn_q8_workspace_bytes(batch: int, h_q: int, h_kv: int, d: int) -> int:
     v = load().sw_decode_attn_q8_workspace_bytes(batch, h_q, h_kv, d)
     if v < 0:

@@ -141,7 +141,7 @@ def test_binding_refuses_what_does_not_fit():
         sw.sparse_attn_decode_q8(torch.zeros((1, 4, 64)), cache, i32[None], i32[:1], i32[None], i32[:1], 4)
     with pytest.raises(sw.SketchWalkError):
         sw.block_tables(i32, i32, 16, torch.zeros((4, 2), dtype=torch.int32), i32, i32[:1], 4)
-    with pytest.raises(sw.SketchWalkError, match="beside k"):
+    with pytest.raises(sw.SketchWalkError, match="d, B"):
         sw.kv_append_q8(x, x, i32, {**cache, "v": cache["k"]})
     with pytest.raises(sw.SketchWalkError, match="k_scale"):
         sw.kv_append_q8(x, x, i32, {**cache, "k_scale": cache["k_scale"][:1]})
