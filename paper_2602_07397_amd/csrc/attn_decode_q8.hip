@@ -41,7 +41,7 @@ __device__ __forceinline__ bf16x8q q8_bf16x8(uint32_t lo, uint32_t hi) {
   return bf16x8q{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-constexpr int kQ8Wgs = 512;                        // workgroups that a call's groups are shared out for
+constexpr int kQ8Wgs = 768;                        // shares of a call, at most
 constexpr int kQ8Batch = 256;                      // sequences of such a call: four a lane
 constexpr int kQ8Splits = 64;                      // workgroups per (sequence, KV head), at most
 
@@ -60,26 +60,40 @@ struct Q8Part {
 
 // How a call's groups are shared out, worked out by every wavefront for itself
 // (no barrier): a workgroup takes a part of one (sequence, head), at most `per`
-// groups, which is a 512th of all and at least one for each of its wavefronts. So
-// sequences of different lengths keep all workgroups equally long, and a
-// workgroup has one prologue and one epilogue.
+// groups, which is a `shares`th of all and at least one for each of its wavefronts.
+// So sequences of different lengths keep all workgroups equally long, and a
+// workgroup has one prologue and one epilogue. Shares: three workgroups per CU in
+// bf16, two in fp32 (16 ragged sequences of up to 16000 tokens, bf16: 19.9 us with
+// 512, 18.1 with 768, 20.7 with 1536; even ones of 65536 69.8, 70.1, 72.1; fp32 of
+// head dimension 64 12.3, 12.5, 12.5).
 struct Q8Plan {
   int lane_before, lane_splits, p[4], c[4], n[4], s[4];
 
   __device__ __forceinline__ void make(int batch, int h_kv, int kmax, int b_max, int B,
-                                       const int32_t* pos, const int32_t* cnt) {
+                                       const int32_t* pos, const int32_t* cnt, uint32_t shares) {
     const int l = threadIdx.x & 63;
+    typedef int i32x4u __attribute__((ext_vector_type(4), aligned(4)));
+    if (4 * l + 4 <= batch) {
+      const i32x4u vp = *reinterpret_cast<const i32x4u*>(pos + 4 * l);
+      const i32x4u vc = *reinterpret_cast<const i32x4u*>(cnt + 4 * l);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int b = 4 * l + i;
-      p[i] = b < batch ? pos[b] : -1;
-      c[i] = b < batch ? cnt[b] : 0;
+      for (int i = 0; i < 4; ++i) {
+        p[i] = vp[i];
+        c[i] = vc[i];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int b = 4 * l + i;
+        p[i] = b < batch ? pos[b] : -1;
+        c[i] = b < batch ? cnt[b] : 0;
+      }
     }
     int sum = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) sum += n[i] = q8_groups(p[i], c[i], kmax, b_max, B);
     const uint32_t T = (uint32_t)__builtin_amdgcn_readlane(wave_inclusive_scan(sum), 63) * h_kv;
-    const uint32_t per = max(4u, (T + kQ8Wgs - 1) / kQ8Wgs);
+    const uint32_t per = max(4u, (T + shares - 1) / shares);
     lane_splits = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -186,7 +200,7 @@ __global__ __launch_bounds__(256) void attn_decode_q8_kernel(
   Q8Part part;
   if constexpr (SHARE) {
     Q8Plan plan;
-    plan.make(batch, h_kv, kmax, b_max, B, pos, cnt);
+    plan.make(batch, h_kv, kmax, b_max, B, pos, cnt, sizeof(T) == 2 ? kQ8Wgs : kQ8Wgs * 2 / 3);
     // for the merge: first workgroup and number of them of each (sequence, head)
     const int b = blockIdx.x;
     if (b < batch && w == 0) {
