@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import importlib.util
 import os
 from typing import Optional, Sequence, Tuple
 
@@ -18,6 +19,7 @@ import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsketchwalk.so")
+HOST_PATH = os.path.join(_HERE, "_host_q8.so")
 
 SW_OK = 0
 SW_F32 = 0
@@ -561,8 +563,7 @@ _U8 = torch.uint8
 
 
 def _at(t: torch.Tensor, dtype: torch.dtype, di: int, name: str) -> int:
-    """Address of a contiguous tensor of ``dtype`` on device ``di``. The calls of a decode
-    step take as long on the host as on the GPU: one test where all is well."""
+    """Address of a contiguous tensor of ``dtype`` on device ``di``."""
     if t.dtype is dtype and t.get_device() == di and t.is_contiguous():
         return t.data_ptr()
     _dev(t, name, dtype)
@@ -581,12 +582,36 @@ def _shaped(t: torch.Tensor, shape: tuple, name: str) -> None:
         raise SketchWalkError(f"{name} of shape {tuple(t.shape)}, {shape} needed")
 
 
-def _gpu(t: torch.Tensor, name: str) -> int:
-    """Index of the GPU that ``t`` is on."""
+_host_module = None
+
+
+def _host():
+    """The native marshalling of the per-layer calls, set up with the library's entry points."""
+    global _host_module
+    if _host_module is None:
+        lib = load()
+        if not os.path.exists(HOST_PATH):
+            raise SketchWalkError(
+                f"{HOST_PATH} is not built; run `python -m paper_2602_07397_amd.build` first")
+        spec = importlib.util.spec_from_file_location("_host_q8", HOST_PATH)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        module.setup(SketchWalkError, {name: ctypes.cast(getattr(lib, name), _vp).value for name in _SIGNATURES})
+        _host_module = module
+    return _host_module
+
+
+def _native(name: str, t: torch.Tensor, *args):
+    """Calls the native function on ``t``'s device and that device's current stream
+    (which refuses tensors that are on no GPU)."""
+    fn = getattr(_host_module or _host(), name)
     di = t.get_device()
     if di < 0:
-        raise SketchWalkError(f"{name} must be a CUDA (HIP) tensor")
-    return di
+        return fn(di, 0, *args)
+    if torch._C._cuda_getDevice() == di:
+        return fn(di, torch._C._cuda_getCurrentRawStream(di), *args)
+    with torch.cuda.device(di):
+        return fn(di, torch._C._cuda_getCurrentRawStream(di), *args)
 
 
 def _launch(di: int, fn, *args) -> None:
@@ -600,23 +625,17 @@ def _launch(di: int, fn, *args) -> None:
         _check(rc, fn.__name__)
 
 
-def _pool(cache: dict, layers: Optional[int] = None):
-    """(device index, n_pages, h_kv, B, d, pointers) of a cache as new_cache_q8 makes it."""
+def _pool(cache: dict, layers: int):
+    """(device index, n_pages, h_kv, B, d, pointers) of a cache of stacked layers."""
     k, v, ks, vs = cache["k"], cache["v"], cache["k_scale"], cache["v_scale"]
     shape = k.shape
     di = k.get_device()
-    if layers is None:
-        fits = len(shape) == 4 and v.shape == (shape[0], shape[1], shape[3], shape[2]) \
-            and ks.shape == shape[:2] and vs.shape == ks.shape
-    else:
-        fits = len(shape) == 5 and shape[0] == layers and v.shape == (*shape[:3], shape[4], shape[3]) \
-            and ks.shape == shape[:3] and vs.shape == ks.shape
-    if not fits:
-        lead = "" if layers is None else f"{layers}, "
+    if not (len(shape) == 5 and shape[0] == layers and v.shape == (*shape[:3], shape[4], shape[3])
+            and ks.shape == shape[:3] and vs.shape == ks.shape):
         raise SketchWalkError(
             f"cache of shapes k {tuple(shape)}, v {tuple(v.shape)}, k_scale {tuple(ks.shape)}, v_scale "
-            f"{tuple(vs.shape)}: ({lead}n_pages, h_kv, B, d), ({lead}n_pages, h_kv, d, B) and twice "
-            f"({lead}n_pages, h_kv) needed")
+            f"{tuple(vs.shape)}: ({layers}, n_pages, h_kv, B, d), ({layers}, n_pages, h_kv, d, B) and twice "
+            f"({layers}, n_pages, h_kv) needed")
     if di < 0:
         raise SketchWalkError("cache k must be a CUDA (HIP) tensor")
     n_pages, h_kv, B, d = shape[-4:]
@@ -631,28 +650,10 @@ def block_tables(old_len: torch.Tensor, new_len: torch.Tensor, B: int, tables: t
     with the stack of free pages (``free_pages`` [n_pages], its height ``n_free`` [1]);
     all int32, the last three updated in place. Returns dict with slots [n_slots],
     cu [n + 1], pos [n] and status [1] (0: done; otherwise nothing changed)."""
-    di = _gpu(tables, "tables")
-    n, b_max = tables.shape
-    p_old = _vec(old_len, n, di, "old_len")
     o = out or {}
-    slots, cu, pos, status = o.get("slots"), o.get("cu"), o.get("pos"), o.get("status")
-    if slots is None:
-        slots = old_len.new_empty(n_slots)
-    if cu is None:
-        cu = old_len.new_empty(n + 1)
-    if pos is None:
-        pos = torch.empty_like(old_len)
-    if status is None:
-        status = old_len.new_empty(1)
-    lib = load()
-    wsb = lib.sw_block_tables_workspace_bytes(n, n_slots)
-    if wsb > 0 and (workspace is None or workspace.numel() < wsb):
-        workspace = old_len.new_empty(wsb, dtype=_U8)
-    p_ws, wsb = (None, 0) if workspace is None else (_at(workspace, _U8, di, "workspace"), workspace.numel())
-    _launch(di, lib.sw_block_tables, n, B, b_max, p_old, _vec(new_len, n, di, "new_len"),
-            _at(tables, _I32, di, "tables"), _at(free_pages, _I32, di, "free_pages"),
-            _vec(n_free, 1, di, "n_free"), free_pages.numel(), rows, n_slots, _vec(slots, n_slots, di, "slots"),
-            _vec(cu, n + 1, di, "cu"), _vec(pos, n, di, "pos"), _vec(status, 1, di, "status"), p_ws, wsb)
+    slots, cu, pos, status = _native("block_tables", tables, old_len, new_len, B, tables, free_pages, n_free,
+                                     n_slots, rows, o.get("slots"), o.get("cu"), o.get("pos"), o.get("status"),
+                                     workspace)
     return {"slots": slots, "cu": cu, "pos": pos, "status": status}
 
 
@@ -661,42 +662,20 @@ def kv_append_q8(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache: d
     """Writes k, v [h_kv][N][d] (bf16 or fp32; heads and tokens in any strides of whole
     16-byte pieces) into the pages of ``slots`` [N]. ``cu`` [n + 1] int32 (device): the
     tokens of a sequence together, in order; without it at most MAX_APPEND_TOKENS."""
-    di, n_pages, h_kv, B, d, pages = _pool(cache)
-    N = slots.numel()
-    shape = (h_kv, N, d)
-    if k.shape != shape or v.shape != shape:
-        raise SketchWalkError(f"k, v of shapes {tuple(k.shape)}, {tuple(v.shape)}: {shape} needed")
-    if k.get_device() != di or v.get_device() != di:
-        raise SketchWalkError(f"k, v on {k.device}, {v.device}, the cache on cuda:{di}")
-    if k.dtype is not v.dtype:
-        raise SketchWalkError("k and v must share a dtype")
-    k_head, k_tok, k_dim = k.stride()
-    v_head, v_tok, v_dim = v.stride()
-    if k_dim != 1 or v_dim != 1:
-        raise SketchWalkError("k and v must be contiguous in their last dimension")
-    n, p_cu = (0, None) if cu is None else (cu.numel() - 1, _at(cu, _I32, di, "cu"))
-    _launch(di, load().sw_kv_append_q8, _dtype_code(k), k.data_ptr(), v.data_ptr(), k_head, k_tok, v_head,
-            v_tok, N, n, p_cu, _at(slots, _I32, di, "slots"), n_pages, h_kv, d, B, *pages)
+    ck = cache["k"]
+    _native("kv_append_q8", ck, k, v, slots, ck, cache["v"], cache["k_scale"], cache["v_scale"], cu)
 
 
 def kv_fetch_q8(cache: dict, tables: torch.Tensor, first: Optional[torch.Tensor], cu: torch.Tensor, N: int,
                 dtype: torch.dtype = torch.bfloat16, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None):
     """K, V [h_kv][N][d] in ``dtype``: positions first[s] .. (``first`` None: 0) of sequence
     s in rows cu[s] .. cu[s + 1] - 1 (device int32). Rows behind cu[n] are not written."""
-    di, n_pages, h_kv, B, d, pages = _pool(cache)
-    n, b_max = tables.shape
-    if out is None:
-        K = torch.empty((h_kv, N, d), dtype=dtype, device=tables.device)
-        V = torch.empty_like(K)
-    else:
-        K, V = out
-        _shaped(K, (h_kv, N, d), "K")
-        _shaped(V, (h_kv, N, d), "V")
-    dt = K.dtype
-    _launch(di, load().sw_kv_fetch_q8, _dtype_code(K), *pages, n_pages, h_kv, d, B, n, b_max,
-            _at(tables, _I32, di, "tables"), None if first is None else _vec(first, n, di, "first"),
-            _vec(cu, n + 1, di, "cu"), N, _at(K, dt, di, "K"), _at(V, dt, di, "V"))
-    return K, V
+    ck = cache["k"]
+    if dtype is not torch.bfloat16 and dtype is not torch.float32:
+        raise SketchWalkError(f"unsupported dtype {dtype}")
+    K, V = (None, None) if out is None else out
+    return _native("kv_fetch_q8", ck, ck, cache["v"], cache["k_scale"], cache["v_scale"], tables, first, cu, N,
+                   SW_BF16 if dtype is torch.bfloat16 else SW_F32, K, V)
 
 
 @functools.lru_cache(maxsize=None)
@@ -713,28 +692,9 @@ def sparse_attn_decode_q8(q: torch.Tensor, cache: dict, tables: torch.Tensor, po
                           workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """sparse_attn_decode over a paged 8-bit cache: q [batch][h_q][d], tables
     [batch][b_max], idx [batch][kmax]."""
-    di, n_pages, h_kv, B, d, pages = _pool(cache)
-    batch, h_q, dq = q.shape
-    if dq != d:
-        raise SketchWalkError(f"q has head dimension {dq}, the cache {d}")
-    rows, b_max = tables.shape
-    if rows != batch:
-        raise SketchWalkError(f"tables of shape {tuple(tables.shape)}, ({batch}, b_max) needed")
-    dt = q.dtype
-    if O is None:
-        O = torch.empty_like(q)
-    else:
-        _shaped(O, (batch, h_q, d), "O")
-    _shaped(idx, (batch, kmax), "idx")
-    wsb = decode_attn_q8_workspace_bytes(batch, h_q, h_kv, d)
-    if wsb > 0 and (workspace is None or workspace.numel() < wsb):
-        workspace = q.new_empty(wsb, dtype=_U8)
-    p_ws, wsb = (None, 0) if workspace is None else (_at(workspace, _U8, di, "workspace"), workspace.numel())
-    _launch(di, load().sw_sparse_attn_decode_q8, _dtype_code(q), _at(q, dt, di, "q"), *pages, batch, h_q, h_kv,
-            d, n_pages, _at(tables, _I32, di, "tables"), b_max, B, _vec(pos, batch, di, "pos"),
-            _at(idx, _I32, di, "idx"), _vec(cnt, batch, di, "cnt"), kmax, float(scale), _at(O, dt, di, "O"),
-            p_ws, wsb)
-    return O
+    ck = cache["k"]
+    return _native("sparse_attn_decode_q8", ck, q, ck, cache["v"], cache["k_scale"], cache["v_scale"], tables, pos,
+                   idx, cnt, kmax, scale, O, workspace)
 
 
 def decode_step_q8(q_new: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, cache: dict,

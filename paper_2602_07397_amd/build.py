@@ -1,4 +1,5 @@
-"""Builds libsketchwalk.so (gfx950) in-tree from csrc/*.hip with hipcc.
+"""Builds libsketchwalk.so (gfx950) in-tree from csrc/*.hip with hipcc, and the
+host module _host_q8.so from csrc/host_q8.cpp with g++.
 
 Usage: python -m paper_2602_07397_amd.build   (or build() from Python)
 """
@@ -9,11 +10,13 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJDIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsketchwalk.so")
+HOST = os.path.join(HERE, "_host_q8.so")
 ARCH = "gfx950"
 
 # Packed-fp32 instructions are disabled for all device code: hipcc -O3 would
@@ -51,12 +54,30 @@ def _compile(src: str) -> str:
     return obj
 
 
+def _build_host() -> None:
+    """The CPython module that marshals the 8-bit cache's calls (host code only)."""
+    import torch
+    from torch.utils.cpp_extension import include_paths, library_paths
+    dirs = [*include_paths(), sysconfig.get_paths()["include"]]
+    libs = library_paths()[0]
+    cmd = ["g++", "-std=c++17", "-O2", "-fPIC", "-shared", "-Wall",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           *(f"-isystem{d}" for d in dirs), os.path.join(CSRC, "host_q8.cpp"), "-o", HOST + ".tmp",
+           f"-L{libs}", f"-Wl,-rpath,{libs}", "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError(f"g++ failed for host_q8.cpp:\n{res.stderr}")
+    os.replace(HOST + ".tmp", HOST)
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(OBJDIR, exist_ok=True)
     srcs = sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".hip"))
     jobs = min(len(srcs), max(1, min(16, os.cpu_count() or 1)))
-    with concurrent.futures.ThreadPoolExecutor(max_workers=jobs) as ex:
+    with concurrent.futures.ThreadPoolExecutor(max_workers=jobs + 1) as ex:
+        host = ex.submit(_build_host)
         objs = list(ex.map(_compile, srcs))
+        host.result()
     tmp = LIB + ".tmp"
     cmd = [_hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *objs]
     res = subprocess.run(cmd, capture_output=True, text=True)

@@ -365,3 +365,45 @@ def test_append_then_fetch_on_another_stream():
     # a stored value is off by at most half a step of its code
     e = pool.e["k"][np.arange(N) // B].T[..., None].astype(np.float64)
     assert np.all(np.abs(K.cpu().double().numpy() - k64) <= np.maximum(np.abs(k64) * 2.0 ** -4, np.exp2(e - 10)))
+
+
+def test_binding_refuses_tensors_that_do_not_fit():
+    h, B, d, P, N = 2, 16, 64, 4, 8
+    cache = sw.new_cache_q8(P, h, B, d, U.DEV)
+    x = torch.zeros((h, N, d), device=U.DEV)
+    slots = torch.arange(N, dtype=torch.int32, device=U.DEV)
+    tables, cu = _i32([[0, 1]]), _i32([0, N])
+    for what, call in {
+        "dtype": lambda: sw.kv_append_q8(x.half(), x.half(), slots, cache),
+        "share": lambda: sw.kv_append_q8(x, x.bfloat16(), slots, cache),
+        "shape": lambda: sw.kv_append_q8(x[:, :4], x, slots, cache),
+        "last dimension": lambda: sw.kv_append_q8(x.transpose(1, 2).contiguous().transpose(1, 2), x, slots, cache),
+        "stride": lambda: sw.kv_append_q8(torch.zeros((h, N, d + 1), device=U.DEV)[..., :d], x, slots, cache),
+        "slots": lambda: sw.kv_append_q8(x, x, slots.long(), cache),
+        "on cpu": lambda: sw.kv_append_q8(x.cpu(), x, slots, cache),
+        "cache k": lambda: sw.kv_append_q8(x, x, slots, {**cache, "k": cache["k"].view(torch.uint8)}),
+        "n_pages": lambda: sw.kv_append_q8(x, x, slots, {**cache, "v": cache["v"][:3]}),
+        "cu": lambda: sw.kv_fetch_q8(cache, tables, None, cu[:1], N),
+        "first": lambda: sw.kv_fetch_q8(cache, tables, _i32([0, 0]), cu, N),
+        "of shape": lambda: sw.kv_fetch_q8(cache, tables, None, cu, N, out=(x[:1], x)),
+        "V must": lambda: sw.kv_fetch_q8(cache, tables, None, cu, N, out=(x, x.bfloat16())),
+        "N=": lambda: sw.kv_fetch_q8(cache, tables, None, cu, -1),
+        "new_len": lambda: sw.block_tables(_i32([0]), _i32([0, 0]), B, tables, _i32([2, 3]), _i32([2]), 4),
+        "contiguous": lambda: sw.block_tables(_i32([0]), _i32([3]), B, _i32([[0, 1], [2, 3]]).t()[:1], _i32([2, 3]),
+                                              _i32([2]), 4),
+    }.items():
+        with pytest.raises(sw.SketchWalkError, match=what):
+            call()
+    q = torch.zeros((1, 4, d), device=U.DEV)
+    args = dict(tables=tables, pos=_i32([5]), idx=_i32([[0]]), cnt=_i32([1]), kmax=1)
+    ok = sw.sparse_attn_decode_q8(q, cache, **args)
+    assert torch.equal(ok, q)                        # an empty cache: zero values
+    for what, change in {"idx": dict(idx=_i32([[0, 1]])), "pos": dict(pos=_i32([5, 5])), "kmax": dict(kmax="1"),
+                         "tables": dict(tables=_i32([0, 1])), "workspace": dict(workspace=torch.zeros(1 << 20, device=U.DEV)),
+                         "O of": dict(O=torch.zeros((1, 2, d), device=U.DEV)),
+                         "O must": dict(O=torch.zeros((1, 4, d), dtype=torch.bfloat16, device=U.DEV)),
+                         "cnt": dict(cnt=torch.ones(1, device=U.DEV))}.items():
+        with pytest.raises(sw.SketchWalkError, match=what):
+            sw.sparse_attn_decode_q8(q, cache, **{**args, **change})
+    with pytest.raises(sw.SketchWalkError, match="q of"):
+        sw.sparse_attn_decode_q8(q[:, :, :32], cache, **args)

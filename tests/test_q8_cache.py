@@ -145,3 +145,9 @@ def test_binding_refuses_what_does_not_fit():
         sw.kv_append_q8(x, x, i32, {**cache, "v": cache["k"]})
     with pytest.raises(sw.SketchWalkError, match="k_scale"):
         sw.kv_append_q8(x, x, i32, {**cache, "k_scale": cache["k_scale"][:1]})
+    with pytest.raises(sw.SketchWalkError, match="CUDA"):
+        sw.kv_append_q8("k", x, i32, cache)          # no tensor
+    with pytest.raises(sw.SketchWalkError, match="integer"):
+        sw.block_tables(i32, i32, 16, torch.zeros((4, 2), dtype=torch.int32), i32, i32[:1], 4.5)
+    with pytest.raises(sw.SketchWalkError, match="dtype"):
+        sw.kv_fetch_q8(cache, i32[None], None, i32[:2], 4, dtype=torch.float16)
