@@ -6,7 +6,7 @@
 //  spread_kernel        pages and slots of calls with many of them
 //  kv_append_q8_kernel  new tokens into the pages their slots name
 //  kv_fetch_q8_kernel   tokens of the cache back as bf16 or fp32
-#include <type_traits>
+#include <climits>
 
 #include "q8.h"
 #include "sw_common.h"
@@ -20,21 +20,33 @@ namespace sw {
 
 constexpr int kTabThreads = 1024;
 
-// Exclusive prefix of v over the workgroup, the sum in *total (two barriers).
-__device__ __forceinline__ int tab_scan(int v, int* tmp, int* total) {
-  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-  const int x = wave_inclusive_scan(v);
-  if (lane == 63) tmp[w] = x;
-  __syncthreads();
-  int before = 0, sum = 0;
+// Exclusive prefixes over the workgroup of three numbers in [0, 2^31) per thread,
+// and their sums, in 64 bits: scans of the lower 20 and the upper bits within
+// each wavefront, then of the wavefronts' sums by every wavefront. One barrier.
+struct TabSums {
+  long long before[3], total[3];
+};
+__device__ __forceinline__ TabSums tab_scan(const int (&v)[3], int (*tmp)[kTabThreads / 64]) {
+  constexpr int W = kTabThreads / 64;
+  const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
+  int part[6], own[6];
 #pragma unroll
-  for (int q = 0; q < kTabThreads / 64; ++q) {
-    before += q < w ? tmp[q] : 0;
-    sum += tmp[q];
+  for (int q = 0; q < 6; ++q) {
+    part[q] = q & 1 ? v[q / 2] >> 20 : v[q / 2] & 0xfffff;
+    own[q] = wave_inclusive_scan(part[q]);
+    if (l == 63) tmp[q][w] = own[q];
   }
-  *total = sum;
   __syncthreads();
-  return before + x - v;
+  TabSums s;
+#pragma unroll
+  for (int q = 0; q < 6; ++q) {
+    const int x = wave_inclusive_scan(l < W ? tmp[q][l] : 0);
+    const int before = w > 0 ? __builtin_amdgcn_readlane(x, w - 1) : 0;
+    const long long b = before + own[q] - part[q], t = __builtin_amdgcn_readlane(x, W - 1);
+    s.before[q / 2] = q & 1 ? s.before[q / 2] + (b << 20) : b;
+    s.total[q / 2] = q & 1 ? s.total[q / 2] + (t << 20) : t;
+  }
+  return s;
 }
 
 // The last i in [0, n) with pre[i] <= k (pre ascending, pre[0] <= k).
@@ -63,132 +75,131 @@ struct TabPlan {
   int32_t* head;      // [2]: whether the call is served, height of the stack before it
 };
 
-// One workgroup. Every length is checked and the pages to give back (R) and to
-// take (A) are counted. If the call can be served whole, the R released pages go
-// onto the stack so that the first of them (sequences ascending, blocks
-// ascending) is on top, and the A new blocks take pages from the top in the same
-// order. Bounded by latency, four dependent loads and a dozen barriers: 4.3 us for
-// one token more for each of 64 requests. PLAN: the prefixes alone, for
-// spread_kernel: pages moved by one workgroup take 1.5 us per 1024, slots as
-// much.
+// tokens >= 0 (in 32 bits: a 64-bit division is over a hundred instructions)
+__device__ __forceinline__ int blocks_of(int tokens, int B) {
+  return (int)(((uint32_t)tokens + (uint32_t)B - 1) / (uint32_t)B);
+}
+
+// One workgroup; a thread has the ceil(n / 1024) sequences from t times that on.
+// Every length is checked and the pages to give back (R) and to take (A) and the
+// new tokens are counted, with one scan. If the call can be served whole, the R
+// released pages go onto the stack so that the first of them (sequences ascending,
+// blocks ascending) is on top, and the A new blocks take pages from the top in the
+// same order. Bounded by latency, three to five dependent loads and as many
+// barriers: 4.6 us for one token more for each of 64 requests. PLAN: the prefixes
+// alone, for spread_kernel (3.4 us for 512 requests): pages moved by one workgroup
+// take 1.5 us per 1024, slots as much.
 template <bool PLAN>
 __global__ __launch_bounds__(kTabThreads) void block_tables_kernel(
     int n_seqs, int B, int b_max, const int32_t* __restrict__ old_len,
     const int32_t* __restrict__ new_len, int32_t* __restrict__ tables, int32_t* __restrict__ free_pages,
     int32_t* __restrict__ n_free, int n_pages, int rows, int n_slots, int32_t* __restrict__ slots,
     int32_t* __restrict__ cu, int32_t* __restrict__ pos, int32_t* __restrict__ status, TabPlan plan) {
-  __shared__ int tmp[kTabThreads / 64];
-  __shared__ int pre[kTabThreads], first[kTabThreads];
-  __shared__ long long sums[3];
-  __shared__ int bad;
+  __shared__ int tmp[6][kTabThreads / 64];
+  __shared__ int pre_r[PLAN ? 1 : kTabThreads], pre_a[PLAN ? 1 : kTabThreads];
   const int t = threadIdx.x;
-  const long long top_len = (long long)b_max * B;
-  if (t < 3) sums[t] = 0;
-  if (t == 0) bad = 0;
-  __syncthreads();
   const int nf = *n_free;
+  const long long top_len = (long long)b_max * B;
+  const int each = (n_seqs + kTabThreads - 1) / kTabThreads;
+  const int s0 = min(t * each, n_seqs), s1 = min(s0 + each, n_seqs);
+  bool wrong = false;
+  int sums[3];
   {
-    long long R = 0, A = 0, grow = 0;
-    bool wrong = false;
-    for (int s = t; s < n_seqs; s += kTabThreads) {
+    long long v[3] = {0, 0, 0};
+    for (int s = s0; s < s1; ++s) {
       const int o = old_len[s], w = new_len[s];
-      wrong |= o < 0 || o > top_len || w < 0 || w > top_len;
-      const int has = (int)((o + (long long)B - 1) / B), need = (int)((w + (long long)B - 1) / B);
-      R += max(has - need, 0);
-      A += max(need - has, 0);
-      grow += max((long long)w - o, 0ll);
-      wrong |= rows > 0 && (long long)w - o > rows;
+      const bool bad = o < 0 || o > top_len || w < 0 || w > top_len || (rows > 0 && (long long)w - o > rows);
+      wrong |= bad;
+      if (bad) continue;
+      const int has = blocks_of(o, B), need = blocks_of(w, B);
+      v[0] += max(has - need, 0);
+      v[1] += max(need - has, 0);
+      v[2] += max(w - o, 0);
     }
-    if (wrong) bad = 1;
-    if (R) atomicAdd((unsigned long long*)&sums[0], (unsigned long long)R);
-    if (A) atomicAdd((unsigned long long*)&sums[1], (unsigned long long)A);
-    if (grow) atomicAdd((unsigned long long*)&sums[2], (unsigned long long)grow);
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+      wrong |= v[q] > INT_MAX;
+      sums[q] = (int)v[q];
+    }
+    if (wrong) sums[0] = sums[1] = sums[2] = 0;
   }
-  __syncthreads();
-  const long long R = sums[0], A = sums[1];
-  const bool valid = !bad && nf >= 0 && nf + R <= n_pages && (rows > 0 || sums[2] <= n_slots);
+  wrong = __syncthreads_or(wrong);
+  const TabSums sc = tab_scan(sums, tmp);
+  const long long R = sc.total[0], A = sc.total[1];
+  const bool valid = !wrong && nf >= 0 && nf + R <= n_pages && (rows > 0 || sc.total[2] <= n_slots);
   const bool ok = valid && A - R <= nf;
   const int top = nf + (int)R;                     // of the stack, after the releases
   if (t == 0) {
     *status = valid ? (ok ? 0 : 1) : 2;
     if (ok) *n_free = top - (int)A;
+    cu[n_seqs] = ok ? (int)sc.total[2] : 0;
     if (PLAN) {
       plan.head[0] = ok;
       plan.head[1] = nf;
-    }
-  }
-  if (!PLAN) {
-    int done_r = 0, done_a = 0;
-    for (int phase = 0; phase < 2 && ok; ++phase) {
-      // 0: releases; 1: allocations
-      if (phase == 0 ? R == 0 : A == 0) continue;
-      for (int s0 = 0; s0 < n_seqs; s0 += kTabThreads) {
-        const int s = s0 + t;
-        int has = 0, need = 0;
-        if (s < n_seqs) {
-          has = (int)((old_len[s] + (long long)B - 1) / B);
-          need = (int)((new_len[s] + (long long)B - 1) / B);
-        }
-        int total;
-        const int k0 = tab_scan(phase == 0 ? max(has - need, 0) : max(need - has, 0), tmp, &total);
-        pre[t] = k0;
-        first[t] = phase == 0 ? need : has;
-        __syncthreads();
-        const int base = phase == 0 ? done_r : done_a;
-        for (int k = t; k < total; k += kTabThreads) {
-          const int i = last_at_most(pre, kTabThreads, k);
-          int32_t* entry = tables + (long long)(s0 + i) * b_max + first[i] + (k - pre[i]);
-          int32_t* item = free_pages + (top - 1 - (base + k));
-          if (phase == 0) {
-            *item = *entry;
-            *entry = -1;
-          } else {
-            *entry = *item;
-          }
-        }
-        if (phase == 0) done_r += total; else done_a += total;
-        __syncthreads();
-      }
+      plan.rel[n_seqs] = (int)R;
+      plan.alc[n_seqs] = (int)A;
     }
   }
   // cumulative new tokens (and pages), positions of the last ones
-  int done_g = 0, done_r = 0, done_a = 0;
-  for (int s0 = 0; s0 < n_seqs; s0 += kTabThreads) {
-    const int s = s0 + t;
-    const int o = s < n_seqs ? old_len[s] : 0, w = s < n_seqs ? new_len[s] : 0;
-    int total;
-    const int g0 = tab_scan(ok ? max(w - o, 0) : 0, tmp, &total);
-    if (s < n_seqs) {
-      cu[s] = done_g + g0;
-      pos[s] = (ok ? w : o) - 1;
-    }
-    done_g += total;
-    if (PLAN) {
-      const int more = ok ? (int)((w + (long long)B - 1) / B) - (int)((o + (long long)B - 1) / B) : 0;
-      const int r0 = tab_scan(max(-more, 0), tmp, &total);
-      if (s < n_seqs) plan.rel[s] = done_r + r0;
-      done_r += total;
-      const int a0 = tab_scan(max(more, 0), tmp, &total);
-      if (s < n_seqs) plan.alc[s] = done_a + a0;
-      done_a += total;
-    }
+  int r = (int)sc.before[0], a = (int)sc.before[1], g = (int)sc.before[2];
+  if (!PLAN) {
+    pre_r[t] = r;
+    pre_a[t] = a;
   }
-  if (t == 0) {
-    cu[n_seqs] = done_g;
+  for (int s = s0; s < s1; ++s) {
+    const int o = old_len[s], w = new_len[s];
+    cu[s] = ok ? g : 0;
+    pos[s] = (ok ? w : o) - 1;
+    if (!ok) continue;
+    const int more = blocks_of(w, B) - blocks_of(o, B);
     if (PLAN) {
-      plan.rel[n_seqs] = done_r;
-      plan.alc[n_seqs] = done_a;
+      plan.rel[s] = r;
+      plan.alc[s] = a;
     }
+    r += max(-more, 0);
+    a += max(more, 0);
+    g += max(w - o, 0);
   }
   if (PLAN) return;
-  __syncthreads();                                 // tables and cu as written above
+  __syncthreads();                                 // the prefixes, and cu for the slots
+  // the sequence of rank k among the blocks given back or taken, and k's number in it
+  auto find = [&](const int* pre, int sign, int k, int* num) {
+    const int i = last_at_most(pre, kTabThreads, k);
+    int s = i * each, left = k - pre[i];
+    for (;; ++s) {
+      const int n = max(sign * (blocks_of(new_len[s], B) - blocks_of(old_len[s], B)), 0);
+      if (left < n) break;
+      left -= n;
+    }
+    *num = left;
+    return s;
+  };
+  if (ok && R > 0) {
+    for (int k = t; k < (int)R; k += kTabThreads) {
+      int j;
+      const int s = find(pre_r, -1, k, &j);
+      int32_t* entry = tables + (long long)s * b_max + blocks_of(new_len[s], B) + j;
+      free_pages[top - 1 - k] = *entry;
+      *entry = -1;
+    }
+    __syncthreads();
+  }
+  if (ok && A > 0) {
+    for (int k = t; k < (int)A; k += kTabThreads) {
+      int j;
+      const int s = find(pre_a, 1, k, &j);
+      tables[(long long)s * b_max + blocks_of(old_len[s], B) + j] = free_pages[top - 1 - k];
+    }
+    __syncthreads();
+  }
+  const int total = ok ? (int)sc.total[2] : 0;
   for (int x = t; x < n_slots; x += kTabThreads) {
     int v = -1;
     if (rows > 0) {
       const int s = x / rows, i = x - s * rows;
       const int o = old_len[s];
       if (ok && i < new_len[s] - o) v = slot_of(tables + (long long)s * b_max, o + i, B, n_pages);
-    } else if (x < done_g) {
+    } else if (x < total) {
       const int s = last_at_most(cu, n_seqs, x);
       v = slot_of(tables + (long long)s * b_max, old_len[s] + (x - cu[s]), B, n_pages);
     }
@@ -196,41 +207,50 @@ __global__ __launch_bounds__(kTabThreads) void block_tables_kernel(
   }
 }
 
-constexpr int kSpreadLds = 2048;                   // prefixes kept in LDS
+constexpr int kSpreadLds = 1024;                   // sequences whose lengths and prefixes are kept in LDS
 
 // Pages and slots of a planned call over many workgroups. 16 lanes take the page
 // of rank k, from the k-th block given back, or off the stack where there is
 // none, and put it into the k-th new block and that block's slots, or onto the
 // stack where there is none: no workgroup reads what another one writes. Slots of
 // the blocks that the sequences had before, and those that stay empty, are
-// written per sequence and behind the last.
+// written per sequence and behind the last. 512 requests, a third of them prompts of
+// 20000 tokens at most: 27000 pages and 1.7 million slots in 7.7 us, 52 with both by
+// one workgroup and a search per slot.
+template <bool LDS>
 __global__ __launch_bounds__(256) void spread_kernel(
     int n_seqs, int B, int b_max, const int32_t* __restrict__ old_len,
     const int32_t* __restrict__ new_len, int32_t* __restrict__ tables, int32_t* __restrict__ free_pages,
     int n_pages, int rows, int n_slots, int32_t* __restrict__ slots, const int32_t* __restrict__ cu,
     TabPlan plan) {
-  __shared__ int rel[kSpreadLds], alc[kSpreadLds];
+  __shared__ int lds[4][LDS ? kSpreadLds : 1];
   const int t = threadIdx.x, lane = t & 15;
   const int unit0 = blockIdx.x * 16 + (t >> 4), units = gridDim.x * 16;
   const long long x0 = (long long)blockIdx.x * 256 + t, xs = (long long)gridDim.x * 256;
-  if (!plan.head[0]) {
+  const int ok = plan.head[0], nf = plan.head[1], R = plan.rel[n_seqs], A = plan.alc[n_seqs];
+  if constexpr (LDS) {
+    for (int s = t; s < n_seqs; s += 256) {
+      lds[0][s] = plan.rel[s];
+      lds[1][s] = plan.alc[s];
+      lds[2][s] = old_len[s];
+      lds[3][s] = new_len[s];
+    }
+    __syncthreads();
+  }
+  auto array = [&](int which, const int32_t* from) {
+    if constexpr (LDS) return static_cast<const int*>(lds[which]);
+    else return from;
+  };
+  const auto rel = array(0, plan.rel), alc = array(1, plan.alc), len0 = array(2, old_len), len1 = array(3, new_len);
+  if (!ok) {
     for (long long x = x0; x < n_slots; x += xs) slots[x] = -1;
     return;
   }
-  const int nf = plan.head[1], R = plan.rel[n_seqs], A = plan.alc[n_seqs];
-  const bool lds = n_seqs <= kSpreadLds;
-  if (lds)
-    for (int s = t; s < n_seqs; s += 256) {
-      rel[s] = plan.rel[s];
-      alc[s] = plan.alc[s];
-    }
-  __syncthreads();
   for (int k = unit0; k < max(R, A); k += units) {
     int page;
     if (k < R) {
-      const int s = lds ? last_at_most(rel, n_seqs, k) : last_at_most(plan.rel, n_seqs, k);
-      const int need = (int)((new_len[s] + (long long)B - 1) / B);
-      int32_t* entry = tables + (long long)s * b_max + need + (k - plan.rel[s]);
+      const int s = last_at_most(rel, n_seqs, k);
+      int32_t* entry = tables + (long long)s * b_max + blocks_of(len1[s], B) + (k - rel[s]);
       page = *entry;
       // every lane has the page before one of them clears the entry
       page = __shfl(page, t & 48);
@@ -242,9 +262,9 @@ __global__ __launch_bounds__(256) void spread_kernel(
       if (lane == 0) free_pages[nf + R - 1 - k] = page;
       continue;
     }
-    const int s = lds ? last_at_most(alc, n_seqs, k) : last_at_most(plan.alc, n_seqs, k);
-    const int o = old_len[s], w = new_len[s];
-    const int j = (int)((o + (long long)B - 1) / B) + (k - plan.alc[s]);
+    const int s = last_at_most(alc, n_seqs, k);
+    const int o = len0[s], w = len1[s];
+    const int j = blocks_of(o, B) + (k - alc[s]);
     if (lane == 0) tables[(long long)s * b_max + j] = page;
     const bool have = (unsigned)page < (unsigned)n_pages;
     const long long out = (rows > 0 ? (long long)s * rows : cu[s]) + ((long long)j * B - o);
@@ -252,9 +272,9 @@ __global__ __launch_bounds__(256) void spread_kernel(
     for (int i = lane; i < n; i += 16) slots[out + i] = have ? page * B + i : -1;
   }
   for (int s = unit0; s < n_seqs; s += units) {
-    const int o = old_len[s], w = new_len[s];
+    const int o = len0[s], w = len1[s];
     const long long out = rows > 0 ? (long long)s * rows : cu[s];
-    const int end = (int)min((long long)w, (o + (long long)B - 1) / B * B);   // of the block it had
+    const int end = (int)min((long long)w, (long long)blocks_of(o, B) * B);   // of the block it had
     if (o < end) {
       const int j = o / B;
       const int page = tables[(long long)s * b_max + j];
@@ -289,8 +309,11 @@ hipError_t launch_block_tables(int n_seqs, int B, int b_max, const int32_t* old_
   hipLaunchKernelGGL(block_tables_kernel<true>, dim3(1), dim3(kTabThreads), 0, st, n_seqs, B, b_max,
                      old_len, new_len, tables, free_pages, n_free, n_pages, rows, n_slots, slots, cu, pos,
                      status, plan);
-  hipLaunchKernelGGL(spread_kernel, dim3(1024), dim3(256), 0, st, n_seqs, B, b_max, old_len, new_len,
-                     tables, free_pages, n_pages, rows, n_slots, slots, cu, plan);
+#define SW_SPREAD(LDS)                                                                             \
+  hipLaunchKernelGGL(spread_kernel<LDS>, dim3(1024), dim3(256), 0, st, n_seqs, B, b_max, old_len,  \
+                     new_len, tables, free_pages, n_pages, rows, n_slots, slots, cu, plan)
+  if (n_seqs <= kSpreadLds) SW_SPREAD(true); else SW_SPREAD(false);
+#undef SW_SPREAD
   return hipGetLastError();
 }
 
