@@ -260,7 +260,7 @@ def test_append_sequences_that_are_skipped_or_empty():
 def test_append_of_extreme_values(dtype):
     """Values at every code and tie, zeros, the ends of the range, infinities and NaN;
     a scale that grows by more than the codes' range."""
-    h, B, d, P = 1, 16, 64, 8
+    h, B, d, P = 1, 16, 64, 9
     cache, pool = sw.new_cache_q8(P, h, B, d, U.DEV), R.Pool(P, h, B, d)
     codes = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).double().numpy()
     codes = np.sort(codes[np.isfinite(codes)])
@@ -277,7 +277,9 @@ def test_append_of_extreme_values(dtype):
             (page(np.concatenate([ties * 2.0 ** -100, [448 * 2.0 ** -100]])), list(range(32, 48))),
             (page([]), list(range(48, 64))), (page([big, -big, 1.0, tiny]), list(range(64, 80))),
             (page([np.inf, -np.inf, np.nan, 3.0, -0.0]), list(range(80, 96))),
-            (page([tiny, -tiny, 3 * tiny]), list(range(96, 112)))]
+            (page([tiny, -tiny, 3 * tiny]), list(range(96, 112))),
+            # below the smallest normal number, where the smallest scale still has codes
+            (page(tiny * np.exp2(-np.arange(9.0)) * 1.5), list(range(128, 144)))]
     for x, slots in rows:
         t = torch.from_numpy(x).to(dtype)
         t64 = t.double().numpy()
@@ -343,6 +345,28 @@ def test_fetch(dtype, h, B, d):
         assert np.all(got[:, cu[-1]:] == 7.0)        # rows behind the last sequence stay
     K0, _ = sw.kv_fetch_q8(cache, torch.from_numpy(tables).to(U.DEV), None, _i32([0, 1, 1, 1, 1, 1]), 1, dtype=dtype)
     np.testing.assert_array_equal(K0.cpu().double().numpy(), pool.tokens("k", tables[0], [0]))
+
+
+def test_fetch_of_every_scale():
+    """Codes times the smallest and the largest scales: exact in fp32; in bf16 exact from
+    2^-133 on, its smallest number (below, rounded to a multiple of it)."""
+    P, h, B, d = 254, 1, 16, 64
+    cache = sw.new_cache_q8(P, h, B, d, U.DEV)
+    codes = torch.arange(256, dtype=torch.uint8)
+    codes[[127, 255]] = 0                            # NaN
+    for n in "kv":
+        cache[n].view(torch.uint8).copy_(codes.repeat(P * B * d // 256).reshape(cache[n].shape))
+        cache[n + "_scale"].copy_(torch.arange(1, 255, dtype=torch.uint8)[:, None])
+    x, _ = R.cache_values(cache)
+    tables, cu = torch.arange(P, dtype=torch.int32, device=U.DEV)[None], _i32([0, P * B])
+    top = float(torch.finfo(torch.float32).max)
+    for dtype, step in ((torch.float32, 2.0 ** -149), (torch.bfloat16, 2.0 ** -133)):
+        K, V = sw.kv_fetch_q8(cache, tables, None, cu, P * B, dtype=dtype)
+        for got, n in ((K, "k"), (V, "v")):
+            want = x[n].transpose(1, 0, 2, 3).reshape(h, P * B, d)
+            want = np.where(np.abs(want) < 2.0 ** -118, np.rint(want / step) * step, want)
+            want = np.where(np.abs(want) > top, np.sign(want) * np.inf, want)
+            np.testing.assert_array_equal(got.cpu().double().numpy(), want)
 
 
 def test_append_then_fetch_on_another_stream():
