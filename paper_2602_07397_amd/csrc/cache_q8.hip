@@ -676,8 +676,12 @@ __global__ __launch_bounds__(256) void kv_fetch_q8_kernel(
   __shared__ long long at4[4];
   __shared__ int off4[4];
   const int t = threadIdx.x, g = blockIdx.y;
+  // Neighbouring tiles go to workgroups 8 apart, which run on one XCD: in blocks of
+  // 128 and more they share the 128-byte lines of the values' rows.
+  int wg = blockIdx.x;
+  if (wg < (int)(gridDim.x & ~15u)) wg = (wg & ~15) + (wg & 7) * 2 + (wg >> 3 & 1);
   int s, c0, c1;
-  const long long u = seq_of_wg(blockIdx.x, n_seqs, cu, kFetchTile, N, &s, &c0, &c1);
+  const long long u = seq_of_wg(wg, n_seqs, cu, kFetchTile, N, &s, &c0, &c1);
   if (c0 >= c1 || u < 0) return;
   const int p0 = first ? max(first[s], 0) : 0;
   const long long pt = (p0 / kFetchTile + u) * kFetchTile;   // the tile's first position
