@@ -475,7 +475,7 @@ int sw_kv_append_q8(int dtype, const void* k, const void* v, int64_t k_head_stri
  * first[s] .. of sequence s into rows cu_seqlens[s] .. cu_seqlens[s+1] - 1 of K
  * and V [h_kv][N][d], the layout that sw_sparse_attn_prefill and
  * sw_sketch_scores take (a cached prefix before a longer prompt). The values are
- * exact. first [n_seqs] int32 may be NULL (0), cu_seqlens int32: both device.
+ * exact (in bf16 from 2^-133, its smallest number, on). first [n_seqs] int32 may be NULL (0), cu_seqlens int32: both device.
  * A position without a page reads as zero; rows behind the last sequence are
  * left as they were.
  */
@@ -494,8 +494,10 @@ int64_t sw_decode_attn_q8_workspace_bytes(int batch, int h_q, int h_kv, int d);
  * idx[b][0..cnt[b]) of sequence b lie in pages tables[b][idx]; tokens behind
  * pos[b] do not count whatever their places hold. Sequences with pos[b] outside
  * [0, b_max * B), and those none of whose selected blocks has a page, get zeros.
- * dtype (q, O) SW_BF16 or SW_F32; h_q / h_kv in [1, 16]; any kmax. fp32 takes q
- * and the weights to 24 bits.
+ * dtype (q, O) SW_BF16 or SW_F32; h_q / h_kv in [1, 16]; any kmax. bf16 rounds the
+ * weights to bf16; fp32 takes q and the weights to 24 bits (queries and values
+ * from 2^-80 in magnitude on). Sums are held in fp32. How the work is shared out,
+ * and so the last bits, depend on the call's lengths.
  */
 int sw_sparse_attn_decode_q8(int dtype, const void* q, const void* k_pages, const void* v_pages,
                              const uint8_t* k_scale, const uint8_t* v_scale, int batch, int h_q,

@@ -114,6 +114,20 @@ def test_attention_at_group_edges(dtype, ctx):
 
 
 @pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("batch,h_q,h_kv,d", [(255, 2, 2, 64), (256, 4, 1, 128), (257, 2, 2, 64), (300, 3, 1, 128)])
+def test_large_batches_of_unlike_lengths(dtype, batch, h_q, h_kv, d):
+    """On both sides of the 256 sequences up to which the work is shared out: one long
+    sequence among short ones and idle ones."""
+    c = _case(batch, batch, h_q, h_kv, d, 16, 1200, dtype, density=0.6)
+    rng = np.random.default_rng(batch)
+    short = rng.integers(-1, 40, size=batch)
+    c["pos"] = [c["pos"][0]] + [int(x) for x in short[1:]]
+    got = _run(c)
+    _check(c, got)
+    assert torch.equal(got, _run(c))
+
+
+@pytest.mark.parametrize("dtype", DT)
 def test_unused_places_may_hold_anything(dtype):
     """Behind a sequence's end, in unlisted pages: NaN codes and the largest values."""
     c = _case(21, 3, 8, 2, 64, 64, 400, dtype)
