@@ -174,6 +174,8 @@ PyObject* kv_append_q8(PyObject* const* a, Py_ssize_t n_args) {
     throw Refused("k, v on " + k.device().str() + ", " + v.device().str() + ", the cache on cuda:" + std::to_string(di));
   if (k.scalar_type() != v.scalar_type()) throw Refused("k and v must share a dtype");
   if (k.stride(2) != 1 || v.stride(2) != 1) throw Refused("k and v must be contiguous in their last dimension");
+  // of a dimension of one entry the stride means nothing
+  auto stride = [](const at::Tensor& x, int64_t dim) { return x.size(dim) > 1 ? x.stride(dim) : 0; };
   const int32_t* p_cu = nullptr;
   int n = 0;
   if (a[9] != Py_None) {
@@ -182,8 +184,8 @@ PyObject* kv_append_q8(PyObject* const* a, Py_ssize_t n_args) {
     n = (int)cu.numel() - 1;
     p_cu = ints(cu, cu.numel(), di, "cu");
   }
-  check(p_append(type_code(k), k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), v.stride(0), v.stride(1), N, n, p_cu,
-                 ints(slots, N, di, "slots"), c.n_pages, c.h_kv, c.d, c.B, c.k, c.v, c.ks, c.vs, stream_of(a[1])),
+  check(p_append(type_code(k), k.data_ptr(), v.data_ptr(), stride(k, 0), stride(k, 1), stride(v, 0), stride(v, 1), N,
+                 n, p_cu, ints(slots, N, di, "slots"), c.n_pages, c.h_kv, c.d, c.B, c.k, c.v, c.ks, c.vs, stream_of(a[1])),
         "sw_kv_append_q8");
   Py_RETURN_NONE;
 }

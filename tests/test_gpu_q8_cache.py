@@ -231,6 +231,20 @@ def test_append_takes_strided_rows_and_many_tokens():
     _same_cache(cache, pool)
 
 
+def test_append_of_one_token_or_head_in_any_stride():
+    rng = np.random.default_rng(15)
+    B, d, P = 16, 64, 3
+    for h, N, shape, stride in ((1, 5, (1, 5, d), (3, d, 1)), (3, 1, (3, 1, d), (d, 5, 1))):
+        base = torch.from_numpy(rng.normal(size=h * N * d)).float().to(U.DEV)
+        k = torch.as_strided(base, shape, stride)
+        v = torch.as_strided(base, shape, stride)
+        slots = [20 + i for i in range(N)]
+        cache, pool = sw.new_cache_q8(P, h, B, d, U.DEV), R.Pool(P, h, B, d)
+        sw.kv_append_q8(k, v, _i32(slots), cache)
+        pool.append(k.cpu().double().numpy(), v.cpu().double().numpy(), slots)
+        _same_cache(cache, pool)
+
+
 def test_append_sequences_that_are_skipped_or_empty():
     rng = np.random.default_rng(6)
     h, B, d, P = 2, 16, 64, 30
