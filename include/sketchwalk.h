@@ -475,9 +475,9 @@ int sw_kv_append_q8(int dtype, const void* k, const void* v, int64_t k_head_stri
  * first[s] .. of sequence s into rows cu_seqlens[s] .. cu_seqlens[s+1] - 1 of K
  * and V [h_kv][N][d], the layout that sw_sparse_attn_prefill and
  * sw_sketch_scores take (a cached prefix before a longer prompt). The values are
- * exact (in bf16 from 2^-133, its smallest number, on). first [n_seqs] int32 may be NULL (0), cu_seqlens int32: both device.
- * A position without a page reads as zero; rows behind the last sequence are
- * left as they were.
+ * exact (in bf16 from 2^-133, its smallest number, on). first [n_seqs] int32 may be
+ * NULL (0), cu_seqlens [n_seqs + 1] int32: both device. A position without a page
+ * reads as zero; rows behind the last sequence are left as they were.
  */
 int sw_kv_fetch_q8(int dtype, const void* k_pages, const void* v_pages, const uint8_t* k_scale,
                    const uint8_t* v_scale, int n_pages, int h_kv, int d, int B, int n_seqs, int b_max,
@@ -511,8 +511,8 @@ int sw_sparse_attn_decode_q8(int dtype, const void* q, const void* k_pages, cons
  * go to `slots` [batch] (as from sw_block_tables with rows = 1; negative: none),
  * the attention reads through tables [batch][b_max]. Pools are stacked over the
  * layers. workspace: >= sw_decode_attn_q8_workspace_bytes(...) bytes, 256-byte
- * aligned (may be NULL when that is 0); with sw_decode_step_q8_workspace_bytes(...) several layers share an
- * attention launch. batch at most SW_MAX_APPEND_TOKENS. The sketch, the walk and
+ * aligned (may be NULL when that is 0); with sw_decode_step_q8_workspace_bytes(...)
+ * several layers share an attention launch. batch at most SW_MAX_APPEND_TOKENS. The sketch, the walk and
  * the selection are those of sw_decode_step, on the tokens as given; results are
  * bit-identical to the per-layer calls.
  */

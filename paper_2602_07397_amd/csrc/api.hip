@@ -646,8 +646,7 @@ int sw_kv_append_q8(int dtype, const void* k, const void* v, int64_t k_head_stri
     return fail(SW_ERR_UNSUPPORTED, "N=%lld tokens without cu_seqlens, at most %d", (long long)N,
                 SW_MAX_APPEND_TOKENS);
   // a launch holds less than 2^32 threads
-  const int64_t wgs = (cu_seqlens ? N / B + 2ll * n_seqs : N) * 2 * h_kv;
-  if (wgs >= (int64_t)1 << 24)
+  if (sw::kv_append_q8_threads(dtype, N, n_seqs, cu_seqlens != nullptr, h_kv, d, B) >= (int64_t)1 << 32)
     return fail(SW_ERR_UNSUPPORTED, "N=%lld tokens of %d sequences and %d heads: too many for one call",
                 (long long)N, cu_seqlens ? n_seqs : 0, h_kv);
   const int64_t strides[4] = {k_head_stride, k_token_stride, v_head_stride, v_token_stride};
@@ -788,6 +787,8 @@ int sw_decode_step_q8(int dtype, int layers, int batch, int h_q, int h_kv, int d
   if (batch > SW_MAX_APPEND_TOKENS)
     return fail(SW_ERR_UNSUPPORTED, "batch=%d, at most %d", batch, SW_MAX_APPEND_TOKENS);
   CHECK(check_pool(n_pages, h_kv, d, B));
+  if (sw::kv_append_q8_threads(dtype, batch, 0, false, h_kv, d, B) >= (int64_t)1 << 32)
+    return fail(SW_ERR_UNSUPPORTED, "batch=%d and %d heads: too many for one call", batch, h_kv);
   CHECK(check_decode_shape(batch, d, r, b_max, B));
   CHECK(check_budget_args(k, density_pct, flags));
   const int need_k = last_row_budget(b_max, k, density_pct, flags);

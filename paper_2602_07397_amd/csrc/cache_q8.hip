@@ -471,7 +471,7 @@ __global__ __launch_bounds__(1024) void kv_append_q8_kernel(
     if (t == 0) leader = 1;
     __syncthreads();
     for (int x = t; x < N; x += nt) {
-      const int o = (x == t ? mine : slots[x]) - base;
+      const int o = (int)((uint32_t)(x == t ? mine : slots[x]) - (uint32_t)base);
       if ((unsigned)o >= (unsigned)B) continue;
       if (x < i) leader = 0;
       else atomicMax(&map[o], x);
@@ -618,6 +618,16 @@ __global__ __launch_bounds__(1024) void kv_append_q8_kernel(
   }
 }
 
+// 64 bytes a thread, whole wavefronts.
+static int append_threads(int dtype, int d, int B) {
+  const int size = dtype == SW_BF16 ? 2 : 4;
+  return (q8_part(B, d, size) * d * size / 64 + 63) / 64 * 64;
+}
+
+long long kv_append_q8_threads(int dtype, int64_t N, int n_seqs, bool by_seq, int h_kv, int d, int B) {
+  return (by_seq ? N / B + 2ll * n_seqs : N) * 2 * h_kv * append_threads(dtype, d, B);
+}
+
 hipError_t launch_kv_append_q8(int dtype, int layers, const void* k, const void* v,
                                const TokenStrides& sd, int N, int n_seqs, const int32_t* cu,
                                const int32_t* slots, int n_pages, int h_kv, int d, int B, void* Kp,
@@ -626,9 +636,8 @@ hipError_t launch_kv_append_q8(int dtype, int layers, const void* k, const void*
   const dim3 grid((unsigned)(wgs * 2 * h_kv), 1, (unsigned)layers);
   uint8_t* kp = static_cast<uint8_t*>(Kp);
   uint8_t* vp = static_cast<uint8_t*>(Vp);
-  // 64 bytes a thread, whole wavefronts
   const int part = q8_part(B, d, dtype == SW_BF16 ? 2 : 4);
-  const int threads = (part * d * (dtype == SW_BF16 ? 2 : 4) / 64 + 63) / 64 * 64;
+  const int threads = append_threads(dtype, d, B);
 #define SW_APPEND_(T, D, SEQ)                                                                      \
   hipLaunchKernelGGL((kv_append_q8_kernel<T, D, SEQ>), grid, dim3((unsigned)threads),              \
                      (unsigned)(D * (part + 4)), st, static_cast<const T*>(k),                     \

@@ -156,6 +156,9 @@ hipError_t launch_block_tables(int n_seqs, int B, int b_max, const int32_t* old_
                                int32_t* n_free, int n_pages, int rows, int n_slots, int32_t* slots,
                                int32_t* cu, int32_t* pos, int32_t* status, int32_t* ws, hipStream_t st);
 
+// Threads of an append's launch along its first dimension.
+long long kv_append_q8_threads(int dtype, int64_t N, int n_seqs, bool by_seq, int h_kv, int d, int B);
+
 // cu NULL: every token by its slot alone.
 hipError_t launch_kv_append_q8(int dtype, int layers, const void* k, const void* v,
                                const TokenStrides& sd, int N, int n_seqs, const int32_t* cu,

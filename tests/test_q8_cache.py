@@ -79,7 +79,9 @@ def test_append_refusals():
     _refused("sw_kv_append_q8", base, {
         "dtype": ({0: 2}, 1, "dtype"), "k": ({1: FAKE + 8}, 1, "k is not"), "v": ({2: None}, 1, "v is NULL"),
         "stride": ({3: 100}, 1, "stride"), "negative": ({4: -1024}, 1, "stride"), "N": ({7: -1}, 1, "N="),
-        "many": ({7: 4097, 9: None}, 2, "4096"), "launch": ({7: 1 << 30, 14: 16}, 2, "too many"), "n_seqs": ({8: 0}, 1, "n_seqs"), "slots": ({10: None}, 1, "slots"),
+        "many": ({7: 4097, 9: None}, 2, "4096"), "launch": ({7: 1 << 30, 14: 16}, 2, "too many"),
+        # 131072 x 2 x 16 workgroups of 1024 threads, 2^32
+        "threads": ({8: 65536, 12: 16, 14: 256}, 2, "too many"), "n_seqs": ({8: 0}, 1, "n_seqs"), "slots": ({10: None}, 1, "slots"),
         "cu": ({9: FAKE + 1}, 1, "cu_seqlens"), "pages": ({11: 0}, 1, "n_pages"), "heads": ({12: 0}, 1, "h_kv"),
         "d": ({13: 96}, 2, "d=96"), "B": ({14: 8}, 1, "B="), "k pages": ({15: FAKE + 4}, 1, "k_pages"),
         "v pages": ({16: None}, 1, "v_pages"), "k scale": ({17: None}, 1, "k_scale"),
@@ -122,6 +124,7 @@ def test_step_refusals():
         "group": ({3: 136}, 2, "h_q/h_kv"), "d": ({5: 256, 6: 64}, 2, "d=256"), "r": ({6: 129}, 1, "r="),
         "pages": ({7: 0}, 1, "n_pages"), "B": ({8: 24}, 1, "B="), "b_max": ({9: 5000}, 1, "b_max"),
         "variant": ({24: 3}, 2, "variant"), "unknown": ({24: 9}, 1, "variant"), "s": ({23: 0}, 1, "s="),
+        "threads": ({2: 4096, 3: 512, 4: 512, 8: 256}, 2, "too many"),
         "budget": ({26: 0}, 1, "density"), "kmax": ({28: 1}, 1, "kmax"), "slots": ({18: None}, 1, "slots"),
         "tables": ({17: None}, 1, "tables"), "state": ({19: FAKE + 8}, 1, "state"),
         "ws bytes": ({35: 100}, 1, "workspace_bytes")})
