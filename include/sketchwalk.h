@@ -439,6 +439,8 @@ int sw_decode_step(int dtype, int layers, int batch, int h_q, int h_kv, int d, i
  *     [0, b_max * B], more new tokens than slots or than rows, or more pages
  *     given back than the pool has. With 1 and 2 nothing changes, cu_seqlens is
  *     0, every slot -1 and pos old_len - 1.
+ * pos is that of a request's last token also where it has no new one:
+ * sw_decode_step_q8 goes by the slots, the calls for a layer by the pos they get.
  * workspace: sw_block_tables_workspace_bytes(...) bytes, 8-byte aligned (may be
  * NULL when that is 0); its contents are scratch. The buffers must not overlap.
  */
@@ -510,9 +512,12 @@ int sw_sparse_attn_decode_q8(int dtype, const void* q, const void* k_pages, cons
  * sw_decode_step_q8 - sw_decode_step over the paged 8-bit cache: the new tokens
  * go to `slots` [batch] (as from sw_block_tables with rows = 1; negative: none),
  * the attention reads through tables [batch][b_max]. Pools are stacked over the
- * layers. workspace: >= sw_decode_attn_q8_workspace_bytes(...) bytes, 256-byte
- * aligned (may be NULL when that is 0); with sw_decode_step_q8_workspace_bytes(...)
- * several layers share an attention launch. batch at most SW_MAX_APPEND_TOKENS. The sketch, the walk and
+ * layers. A sequence without a place for its token (it did not grow, or the tables
+ * could not be served) is idle in every part of the step, as one with pos[b] < 0,
+ * so a captured step without a free page left changes nothing. workspace: >=
+ * sw_decode_attn_q8_workspace_bytes(...) + 4 * batch rounded up to 256 bytes, 256-byte
+ * aligned; with sw_decode_step_q8_workspace_bytes(...) several layers share an
+ * attention launch. batch at most SW_MAX_APPEND_TOKENS. The sketch, the walk and
  * the selection are those of sw_decode_step, on the tokens as given; results are
  * bit-identical to the per-layer calls.
  */

@@ -704,8 +704,8 @@ def decode_step_q8(q_new: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor
                    scale: float = 0.0, out: Optional[dict] = None,
                    workspace: Optional[torch.Tensor] = None) -> dict:
     """decode_step over a paged 8-bit cache of stacked layers: the new tokens go to
-    ``slots`` [batch] (block_tables with rows=1), the attention reads through ``tables``
-    [batch][b_max]. Returns what decode_step returns."""
+    ``slots`` [batch] (block_tables with rows=1; a sequence whose slot is negative is idle),
+    the attention reads through ``tables`` [batch][b_max]. Returns what decode_step returns."""
     L, batch, h_q, d = q_new.shape
     di, n_pages, h_kv, B, dc, pages = _pool(cache, L)
     dev = q_new.device
@@ -731,11 +731,10 @@ def decode_step_q8(q_new: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor
         o["O"] = torch.empty_like(q_new)
     for name, shape in shapes.items():
         _shaped(o[name], shape, name)
-    least = decode_attn_q8_workspace_bytes(batch, h_q, h_kv, d)
-    if least > 0 and (workspace is None or workspace.numel() < least):
+    least = decode_attn_q8_workspace_bytes(batch, h_q, h_kv, d) + (4 * batch + 255) // 256 * 256
+    if workspace is None or workspace.numel() < least:
         wsb = int(load().sw_decode_step_q8_workspace_bytes(batch, h_q, h_kv, d))
         workspace = q_new.new_empty(wsb, dtype=_U8)
-    p_ws, wsb = (None, 0) if workspace is None else (_at(workspace, _U8, di, "workspace"), workspace.numel())
     dt = q_new.dtype
     _launch(di, load().sw_decode_step_q8, _dtype_code(q_new), L, batch, h_q, h_kv, d, r, n_pages, B, b_max,
             _at(q_new, dt, di, "q_new"), _at(k_new, dt, di, "k_new"), _at(v_new, dt, di, "v_new"), *pages,
@@ -743,5 +742,5 @@ def decode_step_q8(q_new: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor
             _vec(pos, batch, di, "pos"), _at(signs, torch.int8, di, "signs"), _at(cols, _I32, di, "cols"), s,
             walk_variant, k, density_pct, flags, kmax, float(scale), _at(o["rows"], torch.float64, di, "rows"),
             _at(o["idx"], _I32, di, "idx"), _at(o["cnt"], _I32, di, "cnt"), _at(o["O"], dt, di, "O"),
-            p_ws, wsb)
+            _at(workspace, _U8, di, "workspace"), workspace.numel())
     return o

@@ -662,7 +662,7 @@ int sw_kv_append_q8(int dtype, const void* k, const void* v, int64_t k_head_stri
   if (cu_seqlens && !aligned(cu_seqlens, 4)) return fail(SW_ERR_INVALID_ARG, "cu_seqlens misaligned");
   const sw::TokenStrides sd{k_head_stride, k_token_stride, v_head_stride, v_token_stride, 0};
   hipError_t e = sw::launch_kv_append_q8(dtype, 1, k, v, sd, (int)N, n_seqs, cu_seqlens, slots, n_pages,
-                                         h_kv, d, B, k_pages, v_pages, k_scale, v_scale,
+                                         h_kv, d, B, k_pages, v_pages, k_scale, v_scale, nullptr, nullptr,
                                          reinterpret_cast<hipStream_t>(stream));
   return hip_status(e, "sw_kv_append_q8 launch");
 }
@@ -759,13 +759,16 @@ int sw_sparse_attn_decode_q8(int dtype, const void* q, const void* k_pages, cons
   return hip_status(e, "sw_sparse_attn_decode_q8 launch");
 }
 
+// Bytes of the sequences' positions at the front of a step's workspace.
+static int64_t live_bytes(int batch) { return ((int64_t)batch * 4 + 255) & ~(int64_t)255; }
+
 // As sw_decode_step_workspace_bytes: eight layers in 64 MiB at most.
 int64_t sw_decode_step_q8_workspace_bytes(int batch, int h_q, int h_kv, int d) {
   const int64_t one = sw_decode_attn_q8_workspace_bytes(batch, h_q, h_kv, d);
-  if (one <= 0) return one;
-  int64_t n = ((int64_t)64 << 20) / one;
+  if (one < 0) return one;
+  int64_t n = one > 0 ? ((int64_t)64 << 20) / one : 0;
   n = n < 1 ? 1 : n > 8 ? 8 : n;
-  return n * one;
+  return live_bytes(batch) + n * one;
 }
 
 int sw_decode_step_q8(int dtype, int layers, int batch, int h_q, int h_kv, int d, int r, int n_pages,
@@ -809,21 +812,23 @@ int sw_decode_step_q8(int dtype, int layers, int batch, int h_q, int h_kv, int d
   CHECK(check_ptr(cnt, 4, "cnt"));
   CHECK(check_ptr(O, 16, "O"));
   const int64_t need = sw_decode_attn_q8_workspace_bytes(batch, h_q, h_kv, d);
-  if (need > 0) {
-    CHECK(check_ptr(workspace, 256, "workspace"));
-    if (workspace_bytes < need)
-      return fail(SW_ERR_INVALID_ARG, "workspace_bytes=%lld < required %lld",
-                  (long long)workspace_bytes, (long long)need);
-  }
+  CHECK(check_ptr(workspace, 256, "workspace"));
+  if (workspace_bytes < live_bytes(batch) + need)
+    return fail(SW_ERR_INVALID_ARG, "workspace_bytes=%lld < required %lld", (long long)workspace_bytes,
+                (long long)(live_bytes(batch) + need));
+  int32_t* live = static_cast<int32_t*>(workspace);   // pos of the sequences that have a new token
+  float* ws = reinterpret_cast<float*>(static_cast<char*>(workspace) + live_bytes(batch));
+  workspace_bytes -= live_bytes(batch);
   if (!(scale > 0.0f)) scale = 1.0f / sqrtf((float)d);
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   const int64_t kv_step = (int64_t)batch * h_kv * d;
   const sw::TokenStrides sd{d, (int64_t)h_kv * d, d, (int64_t)h_kv * d, kv_step};
   hipError_t e = sw::launch_kv_append_q8(dtype, layers, k_new, v_new, sd, batch, 0, nullptr, slots,
-                                         n_pages, h_kv, d, B, k_pages, v_pages, k_scale, v_scale, st);
+                                         n_pages, h_kv, d, B, k_pages, v_pages, k_scale, v_scale, pos,
+                                         live, st);
   if (e != hipSuccess) return hip_status(e, "sw_decode_step_q8 launch");
   e = sw::launch_decode_layers(dtype, layers, q_new, k_new, v_new, nullptr, nullptr, 0, batch, h_q, h_kv,
-                               d, B, pos, signs, cols, r, b_max, static_cast<char*>(state), s,
+                               d, B, live, signs, cols, r, b_max, static_cast<char*>(state), s,
                                walk_variant == SW_WALK_RELU, rows, k, density_pct, flags, idx, cnt, kmax,
                                st);
   if (e != hipSuccess) return hip_status(e, "sw_decode_step_q8 launch");
@@ -836,10 +841,9 @@ int sw_decode_step_q8(int dtype, int layers, int batch, int h_q, int h_kv, int d
     e = sw::launch_attn_decode_q8(dtype, n, static_cast<const char*>(q_new) + l * q_step,
                                   static_cast<const char*>(k_pages) + l * page_step,
                                   static_cast<const char*>(v_pages) + l * page_step, k_scale + l * pool,
-                                  v_scale + l * pool, batch, h_q, h_kv, d, n_pages, tables, b_max, B, pos,
+                                  v_scale + l * pool, batch, h_q, h_kv, d, n_pages, tables, b_max, B, live,
                                   idx + l * batch * kmax, cnt + l * batch, kmax, scale,
-                                  static_cast<char*>(O) + l * q_step, reinterpret_cast<float*>(workspace),
-                                  st);
+                                  static_cast<char*>(O) + l * q_step, ws, st);
     if (e != hipSuccess) return hip_status(e, "sw_decode_step_q8 launch");
   }
   return ok();

@@ -424,12 +424,14 @@ struct Q8Word<float> {
 // maximum to the codes (blocks over 64 KB are read twice), so the workgroup's
 // size goes by the block's: 1024 threads at 64 KB (256 threads with four such
 // pieces each need 250 registers, which halves the wavefronts).
+// live (without SEQ, may be NULL): pos of each token that goes into the cache, -1 of
+// the others.
 template <typename T, int D, bool SEQ>
 __global__ __launch_bounds__(1024) void kv_append_q8_kernel(
     const T* __restrict__ k, const T* __restrict__ v, TokenStrides sd, int N, int n_seqs,
     const int32_t* __restrict__ cu, const int32_t* __restrict__ slots, int n_pages, int h_kv, int B,
     uint8_t* __restrict__ Kp, uint8_t* __restrict__ Vp, uint8_t* __restrict__ ks,
-    uint8_t* __restrict__ vs) {
+    uint8_t* __restrict__ vs, const int32_t* __restrict__ pos, int32_t* __restrict__ live) {
   using W = Q8Word<T>;
   constexpr int V = 16 / (int)sizeof(T);           // elements of a 16-byte piece
   constexpr int PIECES = D / V;                    // of a row
@@ -464,8 +466,9 @@ __global__ __launch_bounds__(1024) void kv_append_q8_kernel(
   } else {
     const int mine = t < N ? slots[t] : -1;        // beside the load of the workgroup's own
     const int i = wg, slot = slots[i];
-    if (slot < 0) return;
     page = slot / B;
+    if (live && hd == 0 && blockIdx.z == 0 && t == 0) live[i] = slot >= 0 && page < n_pages ? pos[i] : -1;
+    if (slot < 0) return;
     const int base = page * B;
     for (int o = t; o < B; o += nt) map[o] = -1;
     if (t == 0) leader = 1;
@@ -631,7 +634,8 @@ long long kv_append_q8_threads(int dtype, int64_t N, int n_seqs, bool by_seq, in
 hipError_t launch_kv_append_q8(int dtype, int layers, const void* k, const void* v,
                                const TokenStrides& sd, int N, int n_seqs, const int32_t* cu,
                                const int32_t* slots, int n_pages, int h_kv, int d, int B, void* Kp,
-                               void* Vp, uint8_t* ks, uint8_t* vs, hipStream_t st) {
+                               void* Vp, uint8_t* ks, uint8_t* vs, const int32_t* pos, int32_t* live,
+                               hipStream_t st) {
   const long long wgs = cu ? (long long)N / B + 2ll * n_seqs : N;
   const dim3 grid((unsigned)(wgs * 2 * h_kv), 1, (unsigned)layers);
   uint8_t* kp = static_cast<uint8_t*>(Kp);
@@ -641,7 +645,8 @@ hipError_t launch_kv_append_q8(int dtype, int layers, const void* k, const void*
 #define SW_APPEND_(T, D, SEQ)                                                                      \
   hipLaunchKernelGGL((kv_append_q8_kernel<T, D, SEQ>), grid, dim3((unsigned)threads),              \
                      (unsigned)(D * (part + 4)), st, static_cast<const T*>(k),                     \
-                     static_cast<const T*>(v), sd, N, n_seqs, cu, slots, n_pages, h_kv, B, kp, vp, ks, vs)
+                     static_cast<const T*>(v), sd, N, n_seqs, cu, slots, n_pages, h_kv, B, kp, vp, ks, vs, \
+                     pos, live)
 #define SW_APPEND(T)                                             \
   do {                                                           \
     if (d == 128) {                                              \

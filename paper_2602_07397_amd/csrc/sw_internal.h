@@ -159,11 +159,13 @@ hipError_t launch_block_tables(int n_seqs, int B, int b_max, const int32_t* old_
 // Threads of an append's launch along its first dimension.
 long long kv_append_q8_threads(int dtype, int64_t N, int n_seqs, bool by_seq, int h_kv, int d, int B);
 
-// cu NULL: every token by its slot alone.
+// cu NULL: every token by its slot alone; live then receives pos of those that have
+// a place, -1 of the others (both may be NULL).
 hipError_t launch_kv_append_q8(int dtype, int layers, const void* k, const void* v,
                                const TokenStrides& sd, int N, int n_seqs, const int32_t* cu,
                                const int32_t* slots, int n_pages, int h_kv, int d, int B, void* Kp,
-                               void* Vp, uint8_t* ks, uint8_t* vs, hipStream_t st);
+                               void* Vp, uint8_t* ks, uint8_t* vs, const int32_t* pos, int32_t* live,
+                               hipStream_t st);
 
 hipError_t launch_kv_fetch_q8(int dtype, const void* Kp, const void* Vp, const uint8_t* ks,
                               const uint8_t* vs, int n_pages, int h_kv, int d, int B, int n_seqs,

@@ -294,7 +294,7 @@ def test_step_is_the_per_layer_calls(dtype, h_q, h_kv, d, B, per_ws):
     kmax = sw.select_max_count_decode(b_max, density_pct=30)
     ws = None
     if per_ws:
-        ws = torch.empty((per_ws * sw.decode_attn_q8_workspace_bytes(n, h_q, h_kv, d),), dtype=torch.uint8, device=U.DEV)
+        ws = torch.empty((256 + per_ws * sw.decode_attn_q8_workspace_bytes(n, h_q, h_kv, d),), dtype=torch.uint8, device=U.DEV)
     for t in range(steps):
         new = [x + 1 for x in lens]
         if t == 2:
@@ -323,6 +323,43 @@ def test_step_is_the_per_layer_calls(dtype, h_q, h_kv, d, B, per_ws):
             assert torch.equal(cache[m].view(torch.uint8), cache2[m].view(torch.uint8)), m
         assert torch.equal(state, state2)
         lens = new
+
+
+@pytest.mark.parametrize("what", ["one", "slot", "pages"])
+def test_step_leaves_sequences_without_a_place_alone(what):
+    """A sequence that did not grow, one whose slot is behind the pool, and a step that the
+    pool could not serve at all: as idle ones, in the cache, the state and the outputs."""
+    L, B, d, h_q, h_kv, prompts = 2, 32, 64, 4, 2, [64, 31, 64]
+    w, ts, tc, pool, cache, state, b_max = _step_setup(torch.float32, h_q, h_kv, d, B, L, prompts, 4, 6)
+    n, P = 3, cache["k"].shape[1]
+    tok = [synth.decode_step_inputs(w, 0, l, batch=n) for l in range(L)]
+    q, k, v = (torch.stack([x[i] for x in tok]).to(U.DEV) for i in range(3))
+    if what == "pages":
+        pool["n_free"].fill_(1)                      # two are needed
+    new = [65, 31 + (what != "one"), 65]
+    bt = sw.block_tables(_i32(prompts), _i32(new), B, pool["tables"], pool["free"], pool["n_free"], n, rows=1)
+    assert int(bt["status"]) == (1 if what == "pages" else 0)
+    if what == "slot":
+        bt["slots"][1] = P * B + 3
+    idle = [0, 1, 2] if what == "pages" else [1]
+    pos = bt["pos"].clone()
+    assert pos[1] >= 0
+    pos[idle] = -1
+    cache2, state2 = {m: t.clone() for m, t in cache.items()}, state.clone()
+    before = state.clone()
+    out = sw.decode_step_q8(q, k, v, cache, pool["tables"], bt["slots"], state, bt["pos"], ts, tc, density_pct=30)
+    slots = bt["slots"].clone()
+    slots[idle] = -1
+    ref = sw.decode_step_q8(q, k, v, cache2, pool["tables"], slots, state2, pos, ts, tc, density_pct=30)
+    assert torch.equal(out["O"], ref["O"]) and torch.all(out["O"][:, idle] == 0)
+    assert torch.equal(state, state2)
+    for m in cache:
+        assert torch.equal(cache[m].view(torch.uint8), cache2[m].view(torch.uint8)), m
+    on = [s for s in range(n) if s not in idle]
+    for m in ("rows", "idx", "cnt"):
+        assert torch.equal(out[m][:, on], ref[m][:, on]), m
+    if not on:
+        assert torch.equal(state, before)
 
 
 def test_step_follows_the_step_over_a_contiguous_cache():

@@ -127,6 +127,8 @@ def test_step_refusals():
         "threads": ({2: 4096, 3: 512, 4: 512, 8: 256}, 2, "too many"),
         "budget": ({26: 0}, 1, "density"), "kmax": ({28: 1}, 1, "kmax"), "slots": ({18: None}, 1, "slots"),
         "tables": ({17: None}, 1, "tables"), "state": ({19: FAKE + 8}, 1, "state"),
+        "workspace": ({34: None, 35: 0}, 1, "workspace"),
+        "ws for the parts alone": ({35: sw.decode_attn_q8_workspace_bytes(4, 32, 8, 128)}, 1, "workspace_bytes"),
         "ws bytes": ({35: 100}, 1, "workspace_bytes")})
 
 
