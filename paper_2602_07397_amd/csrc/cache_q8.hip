@@ -324,29 +324,29 @@ hipError_t launch_block_tables(int n_seqs, int B, int b_max, const int32_t* old_
 // The part of a sequence's tokens that lies in one block. Workgroup w of
 // floor(N / B) + 2 n_seqs finds its own: sequence s has the workgroups from
 // cu[s] / B + 2 s on, which is enough for its floor(n / B) + 2 blocks at most
-// however it lies in them, so no prefix of block counts is needed. Returns the
-// block's number in the sequence's stretch; c0, c1 are the stretch's tokens.
+// however it lies in them, so no prefix of block counts is needed. Every wavefront
+// searches for itself, 64 sequences at a time (one load for up to 64, no
+// barrier). Returns the block's number in the sequence's stretch; c0, c1 are the
+// stretch's tokens.
 __device__ __forceinline__ long long seq_of_wg(int w, int n_seqs, const int32_t* cu, int B, int N,
                                                int* s_out, int* c0, int* c1) {
-  __shared__ int mine[3];
-  const int t = threadIdx.x;
-  if (t == 0) mine[0] = 0, mine[1] = mine[2] = 0;
-  __syncthreads();
-  for (int s0 = 0; s0 < n_seqs; s0 += blockDim.x) {
-    const int s = s0 + t;
-    const int a = cu[min(s, n_seqs)], b = cu[min(s + 1, n_seqs)];
-    // the last sequence that starts at or before w
-    if (s < n_seqs && a / B + 2ll * s <= w && (s + 1 == n_seqs || b / B + 2ll * (s + 1) > w)) {
-      mine[0] = s;
-      mine[1] = a;
-      mine[2] = b;
-    }
-  }
-  __syncthreads();
-  *s_out = mine[0];
-  *c0 = max(mine[1], 0);
-  *c1 = min(mine[2], N);
-  return w - (*c0 / B + 2ll * *s_out);
+  const int l = threadIdx.x & 63;
+  int lo = 0, n = n_seqs, a, b;                    // the last one that starts at or before w
+  do {
+    const int step = (n + 63) / 64, s = lo + l * step;
+    const int at = min(s, n_seqs - 1);
+    const int x = cu[at], y = cu[at + 1];
+    const uint64_t in = __ballot(s < lo + n && x / B + 2ll * s <= w);
+    const int k = in ? 63 - __builtin_clzll(in) : 0;
+    a = __builtin_amdgcn_readlane(x, k);
+    b = __builtin_amdgcn_readlane(y, k);
+    n = min(step, n - k * step);
+    lo += k * step;
+  } while (n > 1);
+  *s_out = lo;
+  *c0 = max(a, 0);
+  *c1 = min(b, N);
+  return w - (*c0 / B + 2ll * lo);
 }
 
 // Tokens of a block that an append workgroup holds in registers at a time: 64 KB,

@@ -361,6 +361,38 @@ def test_fetch(dtype, h, B, d):
     np.testing.assert_array_equal(K0.cpu().double().numpy(), pool.tokens("k", tables[0], [0]))
 
 
+@pytest.mark.parametrize("n", [63, 65, 129, 4097, 5000])
+def test_many_sequences(n):
+    """Append and fetch over more sequences than a wavefront looks at once, most of them short or empty."""
+    rng = np.random.default_rng(n)
+    h, B, d = 1, 16, 64
+    lens = rng.choice([0, 0, 1, 2, 17, 40], size=n)
+    lens[[0, -1]] = [0, 33]
+    starts = rng.integers(0, B, size=n)
+    blocks = -(-(starts + lens) // B) * (lens > 0)
+    cu = np.concatenate([[0], np.cumsum(lens)])
+    first = np.concatenate([[0], np.cumsum(blocks)])
+    P, N = int(first[-1]), int(cu[-1])
+    pages = rng.permutation(P)
+    tables = np.full((n, 4), -1, dtype=np.int32)
+    slots = []
+    for s in range(n):
+        tables[s, :blocks[s]] = pages[first[s]:first[s + 1]]
+        slots += [int(tables[s, p // B]) * B + p % B for p in range(starts[s], starts[s] + lens[s])]
+    cache, pool = sw.new_cache_q8(P, h, B, d, U.DEV), R.Pool(P, h, B, d)
+    k, k64 = _rand(rng, h, N, d, torch.bfloat16)
+    v, v64 = _rand(rng, h, N, d, torch.bfloat16)
+    d_cu = _i32(cu.tolist())
+    sw.kv_append_q8(k.to(U.DEV), v.to(U.DEV), _i32(slots), cache, cu=d_cu)
+    pool.append(k64, v64, slots)
+    _same_cache(cache, pool)
+    K, V = sw.kv_fetch_q8(cache, U.to_dev(tables), _i32(starts.tolist()), d_cu, N, dtype=torch.float32)
+    x, _ = R.cache_values(cache)
+    pg, o = np.array(slots) // B, np.array(slots) % B
+    assert np.array_equal(K.cpu().double().numpy(), x["k"][pg, :, o].transpose(1, 0, 2))
+    assert np.array_equal(V.cpu().double().numpy(), x["v"][pg, :, o].transpose(1, 0, 2))
+
+
 def test_fetch_of_every_scale():
     """Codes times the smallest and the largest scales: exact in fp32; in bf16 exact from
     2^-133 on, its smallest number (below, rounded to a multiple of it)."""
