@@ -215,8 +215,9 @@ constexpr int kSpreadLds = 1024;                   // sequences whose lengths an
 // stack where there is none: no workgroup reads what another one writes. Slots of
 // the blocks that the sequences had before, and those that stay empty, are
 // written per sequence and behind the last. 512 requests, a third of them prompts of
-// 20000 tokens at most: 27000 pages and 1.7 million slots in 7.7 us, 52 with both by
-// one workgroup and a search per slot.
+// 20000 tokens at most: 27000 pages and 1.7 million slots in 7.1 us, 52 with both by
+// one workgroup and a search per slot. Eight workgroups per CU, as many as run at once
+// (four: 7.9 us; sixteen: 7.2).
 template <bool LDS>
 __global__ __launch_bounds__(256) void spread_kernel(
     int n_seqs, int B, int b_max, const int32_t* __restrict__ old_len,
@@ -310,7 +311,7 @@ hipError_t launch_block_tables(int n_seqs, int B, int b_max, const int32_t* old_
                      old_len, new_len, tables, free_pages, n_free, n_pages, rows, n_slots, slots, cu, pos,
                      status, plan);
 #define SW_SPREAD(LDS)                                                                             \
-  hipLaunchKernelGGL(spread_kernel<LDS>, dim3(1024), dim3(256), 0, st, n_seqs, B, b_max, old_len,  \
+  hipLaunchKernelGGL(spread_kernel<LDS>, dim3(2048), dim3(256), 0, st, n_seqs, B, b_max, old_len,  \
                      new_len, tables, free_pages, n_pages, rows, n_slots, slots, cu, plan)
   if (n_seqs <= kSpreadLds) SW_SPREAD(true); else SW_SPREAD(false);
 #undef SW_SPREAD
