@@ -649,7 +649,8 @@ def block_tables(old_len: torch.Tensor, new_len: torch.Tensor, B: int, tables: t
     """Brings ``tables`` [n][b_max] from the requests' old lengths to the new ones,
     with the stack of free pages (``free_pages`` [n_pages], its height ``n_free`` [1]);
     all int32, the last three updated in place. Returns dict with slots [n_slots],
-    cu [n + 1], pos [n] and status [1] (0: done; otherwise nothing changed)."""
+    cu [n + 1], pos [n] and status [1] (0: done; otherwise nothing changed); of ``out``
+    where given, the last three otherwise in one allocation."""
     o = out or {}
     slots, cu, pos, status = _native("block_tables", tables, old_len, new_len, B, tables, free_pages, n_free,
                                      n_slots, rows, o.get("slots"), o.get("cu"), o.get("pos"), o.get("status"),
