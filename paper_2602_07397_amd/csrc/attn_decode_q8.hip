@@ -164,6 +164,11 @@ __device__ __forceinline__ void q8_store(T* O, long long at, float v) {
 //                  8 y + i of chunk lg, that is the lane's own weights as the B
 //                  operand, and for the A operand 16 tokens of a dimension, one
 //                  16-byte piece of the transposed page.
+// bf16: codes and q are bf16 numbers as they are; the weights are rounded to bf16 for
+// the second product (at most 2^-8 of each, as the output at its end; their sum is of the
+// weights before that). Against 64 bits the output is 0.0017 to 0.002 off in the root mean
+// square, 0.0016 to 0.0017 with its own rounding alone; weights in two parts would take the
+// second product twice.
 // fp32: q and the weights go in as sums of three bf16 numbers (24 bits).
 // SHARE: the groups are shared out as Q8Plan does; a (sequence, head) of one
 // workgroup is written out by it, others leave partial sums. Otherwise a
