@@ -164,11 +164,12 @@ __device__ __forceinline__ void q8_store(T* O, long long at, float v) {
 //                  8 y + i of chunk lg, that is the lane's own weights as the B
 //                  operand, and for the A operand 16 tokens of a dimension, one
 //                  16-byte piece of the transposed page.
-// bf16: codes and q are bf16 numbers as they are; the weights are rounded to bf16 for
-// the second product (at most 2^-8 of each, as the output at its end; their sum is of the
-// weights before that). Against 64 bits the output is 0.0017 to 0.002 off in the root mean
-// square, 0.0016 to 0.0017 with its own rounding alone; weights in two parts would take the
-// second product twice.
+// bf16: codes and q are bf16 numbers as they are; the weights go into the second product
+// as sums of two bf16 numbers, at most 2^-16 of each off. One number (2^-8) would take half
+// of that product's instructions and 0.3 to 1.9 % of a call's time (16 sequences of 65536
+// tokens 80.2 us for 80.5, 16 ragged ones of head dimension 64 14.8 for 15.2), but moved
+// the output by 0.0014 in the root mean square; with two it is that of 32-bit weights but for
+// 6e-5, roundings at the end that fall the other way.
 // fp32: q and the weights go in as sums of three bf16 numbers (24 bits).
 // SHARE: the groups are shared out as Q8Plan does; a (sequence, head) of one
 // workgroup is written out by it, others leave partial sums. Otherwise a
@@ -190,7 +191,8 @@ __global__ __launch_bounds__(256) void attn_decode_q8_kernel(
   idx += layer * ls.idx;
   cnt += layer * ls.cnt;
   ws += layer * ls.ws;
-  constexpr int NP = sizeof(T) == 2 ? 1 : 3;       // bf16 parts of q and the weights
+  constexpr int NP = sizeof(T) == 2 ? 1 : 3;       // bf16 parts of q
+  constexpr int NW = sizeof(T) == 2 ? 2 : 3;       // of the weights
   constexpr int NK = D / 64;                       // 16-byte pieces of a key per lane
   constexpr int NT = D / 16;                       // tiles of 16 value dimensions
   __shared__ float sm_o[4][16][D];
@@ -330,7 +332,7 @@ __global__ __launch_bounds__(256) void attn_decode_q8_kernel(
     const float mnew = mx == -INFINITY ? 0.0f : mx;
     const float alpha = q8_exp2(mrun - mnew);
     mrun = mx;
-    bf16x8q pf[NP][2];
+    bf16x8q pf[NW][2];
     float ps = 0.0f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -338,7 +340,7 @@ __global__ __launch_bounds__(256) void attn_decode_q8_kernel(
       ps += pv;
       float x = pv * vf;
 #pragma unroll
-      for (int n2 = 0; n2 < NP; ++n2) {
+      for (int n2 = 0; n2 < NW; ++n2) {
         pf[n2][i / 8][i % 8] = (__bf16)x;
         x -= (float)pf[n2][i / 8][i % 8];
       }
@@ -364,7 +366,7 @@ __global__ __launch_bounds__(256) void attn_decode_q8_kernel(
       const bf16x8q a = q8_bf16x8(r.v[t][0], r.v[t][1]);
       const bf16x8q b = q8_bf16x8(r.v[t][2], r.v[t][3]);
 #pragma unroll
-      for (int i = NP - 1; i >= 0; --i) {
+      for (int i = NW - 1; i >= 0; --i) {
         oacc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pf[i][0], oacc[t], 0, 0, 0);
         oacc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, pf[i][1], oacc[t], 0, 0, 0);
       }

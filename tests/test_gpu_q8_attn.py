@@ -441,3 +441,30 @@ def test_step_captured_replays():
         old.add_(1)
         new.add_(1)
         torch.cuda.synchronize()
+
+
+# --------------------------------------------------------------------------- weights
+
+
+def _fine_bound(c, o, a, top, d, T):
+    """R.attention_bound for weights in two bf16 numbers: the first is off by at most 2^-8
+    of the weight, the second by 2^-8 of what that leaves, so 2^-16 of the weighted mean of
+    |v|; sums and logits as in 32 bits; then the output's own rounding, 2^-8 of it."""
+    return (R.attention_bound(torch.float32, o, a, top, d, T) + 2.0 ** -16 * a) * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(o)
+
+
+@pytest.mark.parametrize("batch,h_q,h_kv,d,B,ctx", [
+    (2, 8, 2, 128, 64, 50), (3, 8, 2, 64, 16, 700), (2, 16, 1, 128, 128, 9000), (260, 4, 2, 64, 16, 40)])
+def test_bf16_weights_keep_16_bits(batch, h_q, h_kv, d, B, ctx):
+    """Outputs that are small against the values they are made of show what the weights lose."""
+    c = _case(batch + ctx, batch, h_q, h_kv, d, B, ctx, torch.bfloat16)
+    got = _run(c).double().cpu().numpy()
+    x, _ = R.cache_values(c["cache"])
+    for b in range(batch):
+        pages, places = _selected(c, b)
+        K = x["k"][pages, :, places].transpose(1, 0, 2)
+        V = x["v"][pages, :, places].transpose(1, 0, 2)
+        o, a, top = R.attention(c["q"][b].double().numpy(), K, V, 1.0 / math.sqrt(d))
+        err = np.abs(got[b] - o)
+        bound = _fine_bound(c, o, a, top, d, len(pages))
+        assert np.all(err <= bound), (b, float((err / bound).max()))
