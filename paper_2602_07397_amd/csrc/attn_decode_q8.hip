@@ -135,6 +135,10 @@ struct Q8Plan {
   }
 };
 
+// The output of a (sequence, head) whose largest logit is -infinity: 0 without a token
+// (a sum of weights of 0), NaN otherwise.
+__device__ __forceinline__ float q8_no_max(float l) { return l == 0.0f ? 0.0f : NAN; }
+
 // The workspace of a layer, in floats: first workgroup and number of them of each
 // (sequence, head); then of every workgroup its heads' maxima and sums of weights,
 // and their outputs (16-byte aligned).
@@ -166,7 +170,7 @@ __device__ __forceinline__ void q8_store(T* O, long long at, float v) {
 //                  16-byte piece of the transposed page.
 // bf16: codes and q are bf16 numbers as they are; the weights go into the second product
 // as sums of two bf16 numbers, at most 2^-16 of each off. One number (2^-8) would take half
-// of that product's instructions and 0.3 to 1.9 % of a call's time (16 sequences of 65536
+// of that product's instructions and 0.3 to 2.5 % of a call's time (16 sequences of 65536
 // tokens 80.2 us for 80.5, 16 ragged ones of head dimension 64 14.8 for 15.2), but moved
 // the output by 0.0014 in the root mean square; with two it is that of 32-bit weights but for
 // 6e-5, roundings at the end that fall the other way.
@@ -265,6 +269,7 @@ __global__ __launch_bounds__(256) void attn_decode_q8_kernel(
 #pragma unroll
   for (int t = 0; t < NT; ++t) oacc[t] = f32x4q{0.f, 0.f, 0.f, 0.f};
   float mrun = -INFINITY, lrun = 0.0f;
+  bool seen = false;                               // a token that counts
   // the lane's chunk of the listed groups: page, first token (INT_MAX: none of it
   // counts), place in the page
   int c_page = 0, c_t0 = INT_MAX, c_off = 0;
@@ -346,6 +351,7 @@ __global__ __launch_bounds__(256) void attn_decode_q8_kernel(
       }
     }
     lrun = lrun * alpha + ps;
+    seen |= r.t0 <= p;
     // places that do not count may hold any code, NaN among them
     const int left = r.t0 <= p ? min(p - r.t0 + 1, 16) : 0;   // tokens of the chunk that count
     if (__any(left < 16)) {
@@ -395,12 +401,15 @@ __global__ __launch_bounds__(256) void attn_decode_q8_kernel(
     }
   }
   // per-wave partials: head ln; lane groups hold disjoint tokens (sum l) and
-  // disjoint output dims
+  // disjoint output dims. A maximum of -infinity is that of no token, or of tokens
+  // whose logits are all NaN or -infinity, for which the softmax has no value: a sum of
+  // weights that is not 0 tells them apart (beside finite logits the latter weigh 0).
   const float lsum = q8_xsum(lrun);
+  const float none = __any(seen) && mrun == -INFINITY ? 1.0f : 0.0f;
   if (ln < G) {
     if (lg == 0) {
       sm_m[w][ln] = mrun;
-      sm_l[w][ln] = lsum;
+      sm_l[w][ln] = lsum + none;
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t)
@@ -424,10 +433,13 @@ __global__ __launch_bounds__(256) void attn_decode_q8_kernel(
         Lsum += sm_l[k][u] * sc;
         Osum += *reinterpret_cast<const f32x4q*>(&sm_o[k][u][dim]) * sc;
       }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) Lsum += sm_l[k][u];
     }
     if (part.splits == 1) {
       const long long at = ((long long)bi * h_q + g * G + u) * D + dim;
-      const float inv = Lsum != 0.0f ? 1.0f / Lsum : 0.0f;
+      const float inv = M == -INFINITY ? q8_no_max(Lsum) : 1.0f / Lsum;
       if constexpr (sizeof(T) == 2)
         *reinterpret_cast<uint2*>(O + at) =
             make_uint2(pack_bf16x2(Osum[0] * inv, Osum[1] * inv), pack_bf16x2(Osum[2] * inv, Osum[3] * inv));
@@ -489,17 +501,17 @@ __global__ __launch_bounds__(256) void attn_merge_q8_kernel(const float* __restr
   const float2 ml = *reinterpret_cast<const float2*>(ws + q8_ws_sums(pairs) + ((seg + min(l, S - 1)) * G + u) * 2);
   const float* o = ws + q8_ws_outs(pairs, G) + (seg * G + u) * D + l * V;
   vec acc = {};
-  float Lsum;
+  float top, Lsum;
   auto add = [&](auto n) {
     constexpr int N = decltype(n)::value;
     vec x[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] = *reinterpret_cast<const vec*>(o + (long long)min(w + 4 * i, S - 1) * G * D);
     const float m = l < S ? ml.x : -INFINITY;
-    const float M = q8_wave_max(m);
-    // without any token all weigh 0
-    const float sc = M != -INFINITY && l < S ? q8_exp2(m - M) : 0.0f;
-    Lsum = q8_wave_sum(l < S ? ml.y * sc : 0.0f);
+    top = q8_wave_max(m);
+    // without a maximum the outputs weigh 0, the sums of weights 1 (whether there is a token)
+    const float sc = top != -INFINITY && l < S ? q8_exp2(m - top) : 0.0f;
+    Lsum = q8_wave_sum(l < S ? ml.y * (top != -INFINITY ? sc : 1.0f) : 0.0f);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int s = w + 4 * i;
@@ -513,7 +525,7 @@ __global__ __launch_bounds__(256) void attn_merge_q8_kernel(const float* __restr
   __syncthreads();
   if (t >= D) return;
   const float sum = ((part[0][t] + part[1][t]) + part[2][t]) + part[3][t];
-  q8_store(O, at + t, Lsum != 0.0f ? sum / Lsum : 0.0f);
+  q8_store(O, at + t, top == -INFINITY ? q8_no_max(Lsum) : sum / Lsum);
 }
 
 int64_t attn_decode_q8_workspace_bytes(int batch, int h_q, int h_kv, int d) {

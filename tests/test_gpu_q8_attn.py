@@ -468,3 +468,62 @@ def test_bf16_weights_keep_16_bits(batch, h_q, h_kv, d, B, ctx):
         err = np.abs(got[b] - o)
         bound = _fine_bound(c, o, a, top, d, len(pages))
         assert np.all(err <= bound), (b, float((err / bound).max()))
+
+
+# --------------------------------------------------------------------------- NaN and rows without a token
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("batch,ctx", [(1, 9000), (3, 40), (260, 70)])
+def test_a_query_that_is_not_finite_shows(batch, ctx, dtype):
+    """Over split work, one workgroup, and batches that are not shared out: a NaN in a query
+    makes its head NaN, other heads keep their bits; rows without a token stay zero."""
+    c = _case(41, batch, 8, 2, 64, 16, ctx, dtype)
+    if batch > 1:
+        c["pos"][1] = -1
+    clean = _run(c)
+    assert torch.isfinite(clean).all()
+    c["q"] = c["q"].clone()
+    c["q"][:, 3, 7] = math.nan
+    got = _run(c)
+    live = [b for b in range(batch) if c["pos"][b] >= 0]
+    assert torch.isnan(got[live, 3]).all()
+    rest = [u for u in range(8) if u != 3]
+    assert torch.equal(got[:, rest], clean[:, rest])
+    if batch > 1:
+        assert torch.all(got[1] == 0)
+
+
+@pytest.mark.parametrize("dtype", DT)
+def test_tokens_that_are_all_nan_show(dtype):
+    """A first token whose key was infinite (stored as NaN), and contexts of such keys."""
+    h, B, d = 2, 16, 64
+    cache = sw.new_cache_q8(40, h, B, d, U.DEV)
+    n = 33 * B
+    k = torch.full((h, n, d), math.inf, dtype=dtype, device=U.DEV)
+    v = torch.ones((h, n, d), dtype=dtype, device=U.DEV)
+    sw.kv_append_q8(k, v, torch.arange(n, dtype=torch.int32, device=U.DEV), cache, cu=_i32([0, n]))
+    tables = torch.arange(33, dtype=torch.int32, device=U.DEV).repeat(2, 1)
+    idx = tables.clone()
+    q = torch.ones((2, 4, d), dtype=dtype, device=U.DEV)
+    for pos in ([0, -1], [n - 1, 5], [-1, n - 1]):
+        got = sw.sparse_attn_decode_q8(q, cache, tables, _i32(pos), idx, _i32([33, 33]), 33)
+        for b in range(2):
+            assert (torch.isnan(got[b]) if pos[b] >= 0 else got[b] == 0).all(), pos
+
+
+@pytest.mark.parametrize("dtype", DT)
+def test_logits_that_are_all_minus_infinity(dtype):
+    """The softmax of such a row has no value; of one with a finite logit beside them it has."""
+    h, B, d = 1, 16, 64
+    cache = sw.new_cache_q8(40, h, B, d, U.DEV)
+    n = 33 * B
+    k = torch.ones((h, n, d), dtype=dtype, device=U.DEV)
+    v = torch.randn((h, n, d), dtype=dtype, device=U.DEV)
+    sw.kv_append_q8(k, v, torch.arange(n, dtype=torch.int32, device=U.DEV), cache, cu=_i32([0, n]))
+    tables = torch.arange(33, dtype=torch.int32, device=U.DEV)[None]
+    q = torch.ones((1, 4, d), dtype=dtype, device=U.DEV)
+    q[0, 1, 3] = -math.inf
+    for pos in (0, 16, n - 1):
+        got = sw.sparse_attn_decode_q8(q, cache, tables, _i32([pos]), tables, _i32([33]), 33)
+        assert torch.isnan(got[0, 1]).all() and torch.isfinite(got[0, [0, 2, 3]]).all(), pos
