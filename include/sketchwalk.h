@@ -494,9 +494,10 @@ int64_t sw_decode_attn_q8_workspace_bytes(int batch, int h_q, int h_kv, int d);
  * sw_sparse_attn_decode_q8 - sw_sparse_attn_decode over the paged 8-bit cache:
  * the same attention with the keys and values that the codes stand for. Blocks
  * idx[b][0..cnt[b]) of sequence b lie in pages tables[b][idx]; tokens behind
- * pos[b] do not count whatever their places hold. Sequences with pos[b] outside
- * [0, b_max * B), and those none of whose selected blocks has a page, get zeros; a
- * head whose tokens' logits are all NaN or -infinity gets NaN.
+ * pos[b] do not count whatever their places hold, nor do other pages and their
+ * scales. Sequences with pos[b] outside [0, b_max * B), and those none of whose
+ * selected blocks has a page, get zeros; a head whose tokens' logits are all NaN or
+ * -infinity gets NaN.
  * dtype (q, O) SW_BF16 or SW_F32; h_q / h_kv in [1, 16]; any kmax. bf16 takes the
  * weights to 16 bits; fp32 takes q and the weights to 24 bits (queries and values
  * from 2^-80 in magnitude on). Sums are held in fp32. How the work is shared out,

@@ -324,7 +324,8 @@ __global__ __launch_bounds__(256) void attn_decode_q8_kernel(
         }
       }
     }
-    const float kf = q8_scale(r.ks) * sl2, vf = q8_scale(r.vs);
+    // a chunk that does not count has the scale of some page, maybe one never begun
+    const float kf = q8_scale(r.ks) * sl2, vf = r.t0 <= p ? q8_scale(r.vs) : 0.0f;
     float sv[16];
     float mx = -INFINITY;
 #pragma unroll

@@ -527,3 +527,23 @@ def test_logits_that_are_all_minus_infinity(dtype):
     for pos in (0, 16, n - 1):
         got = sw.sparse_attn_decode_q8(q, cache, tables, _i32([pos]), tables, _i32([33]), 33)
         assert torch.isnan(got[0, 1]).all() and torch.isfinite(got[0, [0, 2, 3]]).all(), pos
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("batch", [3, 260])
+def test_unlisted_pages_may_have_any_scale(batch, dtype):
+    """Pages of no listed block were never begun: their scales, page 0's among them, hold any byte."""
+    c = _case(28, batch, 8, 2, 64, 64, 400, dtype)
+    c["pos"][1] = -1
+    c["cnt"][2] = 1                                  # one group, not full
+    c["pos"][2] = 9
+    c["tables"][c["tables"] == 0] = c["P"] - 1       # page 0 is nobody's
+    clean = _run(c)
+    _check(c, clean)
+    used = sorted({pg for b in range(batch) for pg in _selected(c, b)[0]})
+    rest = sorted(set(range(c["P"])) - set(used))
+    assert rest[0] == 0
+    for byte in (255, 254, 0):
+        for n in "kv":
+            c["cache"][n + "_scale"][rest] = byte
+        assert torch.equal(clean, _run(c)), byte
