@@ -436,9 +436,9 @@ int sw_decode_step(int dtype, int layers, int batch, int h_q, int h_kv, int d, i
  *   cu_seqlens [n_seqs + 1] int32 (out): cumulative numbers of new tokens
  *   pos [n_seqs] int32 (out): position of the last token, new_len - 1
  *   status [1] int32 (out): 0; 1: too few free pages; 2: a length outside
- *     [0, b_max * B], more new tokens than slots or than rows, or more pages
- *     given back than the pool has. With 1 and 2 nothing changes, cu_seqlens is
- *     0, every slot -1 and pos old_len - 1.
+ *     [0, b_max * B], more new tokens than slots or than rows, a block given back
+ *     that has no page, or more pages given back than the pool has. With 1 and 2
+ *     nothing changes, cu_seqlens is 0, every slot -1 and pos old_len - 1.
  * pos is that of a request's last token also where it has no new one:
  * sw_decode_step_q8 goes by the slots, the calls for a layer by the pos they get.
  * workspace: sw_block_tables_workspace_bytes(...) bytes, 8-byte aligned (may be

@@ -69,15 +69,60 @@ __device__ __forceinline__ int slot_of(const int32_t* table, int p, int B, int n
 
 // What the workgroups of a spread call need of the plan: the pages that the
 // sequences before each one give back and take, and the stack.
+constexpr int kTabCheck = 32;                      // workgroups that look at the blocks given back
 struct TabPlan {
   int32_t* rel;       // [n_seqs + 1]
   int32_t* alc;       // [n_seqs + 1]
-  int32_t* head;      // [2]: whether the call is served, height of the stack before it
+  int32_t* head;      // [2]: whether the lengths can be served, height of the stack before the call
+  int32_t* holes;     // [kTabCheck]: whether a block given back is without a page
 };
 
 // tokens >= 0 (in 32 bits: a 64-bit division is over a hundred instructions)
 __device__ __forceinline__ int blocks_of(int tokens, int B) {
   return (int)(((uint32_t)tokens + (uint32_t)B - 1) / (uint32_t)B);
+}
+
+// Lengths that no call is served with.
+__device__ __forceinline__ bool bad_lengths(int o, int w, long long top_len, int rows) {
+  return o < 0 || o > top_len || w < 0 || w > top_len || (rows > 0 && (long long)w - o > rows);
+}
+
+// Whether a block that is given back is without a page, in any lane of the wavefront:
+// `wave` of `waves` looks at sequences wave, wave + waves, ..., the first 64 blocks of
+// four of them on their way at a time.
+__device__ __forceinline__ bool without_page(int wave, int waves, int n_seqs, int B, int b_max, int rows,
+                                             const int32_t* old_len, const int32_t* new_len,
+                                             const int32_t* tables, int n_pages) {
+  constexpr int N = 4;
+  const int l = threadIdx.x & 63;
+  uint32_t top = 0;                                // the entries as unsigned numbers
+  for (long long base = wave; base < n_seqs; base += 64ll * waves) {
+    const long long s = base + (long long)l * waves;
+    const int o = s < n_seqs ? old_len[s] : 0, w = s < n_seqs ? new_len[s] : 0;
+    const int first = blocks_of(w, B), end = blocks_of(o, B);
+    uint64_t left = __ballot(!bad_lengths(o, w, (long long)b_max * B, rows) && first < end);
+    while (left) {
+      const int32_t* row[N];
+      int size[N], who = 0;
+      uint32_t page[N];
+#pragma unroll
+      for (int q = 0; q < N; ++q) {
+        if (left) who = __builtin_ctzll(left);     // then the last one again
+        left &= left - 1;
+        const int a = __builtin_amdgcn_readlane(first, who);
+        size[q] = __builtin_amdgcn_readlane(end, who) - a;
+        row[q] = tables + (base + (long long)who * waves) * b_max + a;
+        page[q] = (uint32_t)row[q][min(l, size[q] - 1)];
+      }
+#pragma unroll
+      for (int q = 0; q < N; ++q) {
+        top = max(top, page[q]);
+#pragma unroll 4
+        for (int j = 64 + l; j < size[q]; j += 64) top = max(top, (uint32_t)row[q][j]);
+      }
+    }
+  }
+  return __any(top >= (uint32_t)n_pages);
 }
 
 // One workgroup; a thread has the ceil(n / 1024) sequences from t times that on.
@@ -88,7 +133,11 @@ __device__ __forceinline__ int blocks_of(int tokens, int B) {
 // same order. Bounded by latency, three to five dependent loads and as many
 // barriers: 4.6 us for one token more for each of 64 requests. PLAN: the prefixes
 // alone, for spread_kernel (3.4 us for 512 requests): pages moved by one workgroup
-// take 1.5 us per 1024, slots as much.
+// take 1.5 us per 1024, slots as much. A block given back has to have a page: the
+// workgroup looks at them itself where there are any (64 requests, a step of one token and the
+// same step back in turn: 4.6 -> 5.0 us a call); PLAN: kTabCheck workgroups beside it, and
+// spread_kernel at what they found (512 requests, 8000 to 27000 blocks given back: 10.1 -> 11.1
+// for the two launches; 14.9 with the check in the planning workgroup).
 template <bool PLAN>
 __global__ __launch_bounds__(kTabThreads) void block_tables_kernel(
     int n_seqs, int B, int b_max, const int32_t* __restrict__ old_len,
@@ -98,6 +147,14 @@ __global__ __launch_bounds__(kTabThreads) void block_tables_kernel(
   __shared__ int tmp[6][kTabThreads / 64];
   __shared__ int pre_r[PLAN ? 1 : kTabThreads], pre_a[PLAN ? 1 : kTabThreads];
   const int t = threadIdx.x;
+  if (PLAN && blockIdx.x > 0) {
+    const int x = blockIdx.x - 1;
+    const bool hole = without_page(x * (kTabThreads / 64) + (t >> 6), kTabCheck * (kTabThreads / 64), n_seqs, B,
+                                   b_max, rows, old_len, new_len, tables, n_pages);
+    const bool any = __syncthreads_or(hole);
+    if (t == 0) plan.holes[x] = any;
+    return;
+  }
   const int nf = *n_free;
   const long long top_len = (long long)b_max * B;
   const int each = (n_seqs + kTabThreads - 1) / kTabThreads;
@@ -108,7 +165,7 @@ __global__ __launch_bounds__(kTabThreads) void block_tables_kernel(
     long long v[3] = {0, 0, 0};
     for (int s = s0; s < s1; ++s) {
       const int o = old_len[s], w = new_len[s];
-      const bool bad = o < 0 || o > top_len || w < 0 || w > top_len || (rows > 0 && (long long)w - o > rows);
+      const bool bad = bad_lengths(o, w, top_len, rows);
       wrong |= bad;
       if (bad) continue;
       const int has = blocks_of(o, B), need = blocks_of(w, B);
@@ -126,6 +183,9 @@ __global__ __launch_bounds__(kTabThreads) void block_tables_kernel(
   wrong = __syncthreads_or(wrong);
   const TabSums sc = tab_scan(sums, tmp);
   const long long R = sc.total[0], A = sc.total[1];
+  if (!PLAN && R > 0)
+    wrong |= __syncthreads_or(without_page(t >> 6, kTabThreads / 64, n_seqs, B, b_max, rows, old_len, new_len,
+                                           tables, n_pages));
   const bool valid = !wrong && nf >= 0 && nf + R <= n_pages && (rows > 0 || sc.total[2] <= n_slots);
   const bool ok = valid && A - R <= nf;
   const int top = nf + (int)R;                     // of the stack, after the releases
@@ -222,13 +282,14 @@ template <bool LDS>
 __global__ __launch_bounds__(256) void spread_kernel(
     int n_seqs, int B, int b_max, const int32_t* __restrict__ old_len,
     const int32_t* __restrict__ new_len, int32_t* __restrict__ tables, int32_t* __restrict__ free_pages,
-    int n_pages, int rows, int n_slots, int32_t* __restrict__ slots, const int32_t* __restrict__ cu,
-    TabPlan plan) {
+    int32_t* __restrict__ n_free, int n_pages, int rows, int n_slots, int32_t* __restrict__ slots,
+    int32_t* __restrict__ cu, int32_t* __restrict__ pos, int32_t* __restrict__ status, TabPlan plan) {
   __shared__ int lds[4][LDS ? kSpreadLds : 1];
   const int t = threadIdx.x, lane = t & 15;
   const int unit0 = blockIdx.x * 16 + (t >> 4), units = gridDim.x * 16;
   const long long x0 = (long long)blockIdx.x * 256 + t, xs = (long long)gridDim.x * 256;
   const int ok = plan.head[0], nf = plan.head[1], R = plan.rel[n_seqs], A = plan.alc[n_seqs];
+  const bool hole = __any(plan.holes[t % kTabCheck]);
   if constexpr (LDS) {
     for (int s = t; s < n_seqs; s += 256) {
       lds[0][s] = plan.rel[s];
@@ -243,8 +304,19 @@ __global__ __launch_bounds__(256) void spread_kernel(
     else return from;
   };
   const auto rel = array(0, plan.rel), alc = array(1, plan.alc), len0 = array(2, old_len), len1 = array(3, new_len);
-  if (!ok) {
+  if (!ok || hole) {
     for (long long x = x0; x < n_slots; x += xs) slots[x] = -1;
+    if (!hole) return;
+    // refused after the plan was made
+    for (long long s = x0; s < n_seqs; s += xs) {
+      cu[s] = 0;
+      pos[s] = old_len[s] - 1;
+    }
+    if (x0 == 0) {
+      cu[n_seqs] = 0;
+      *n_free = nf;
+      *status = 2;
+    }
     return;
   }
   for (int k = unit0; k < max(R, A); k += units) {
@@ -293,7 +365,7 @@ __global__ __launch_bounds__(256) void spread_kernel(
 constexpr long long kTabOneLaunch = 4 * kTabThreads;
 
 int64_t block_tables_workspace_bytes(int n_seqs, int64_t n_slots) {
-  return n_slots <= kTabOneLaunch ? 0 : 8ll * (n_seqs + 2);
+  return n_slots <= kTabOneLaunch ? 0 : 8ll * (n_seqs + 2) + 4 * kTabCheck;
 }
 
 hipError_t launch_block_tables(int n_seqs, int B, int b_max, const int32_t* old_len,
@@ -306,13 +378,14 @@ hipError_t launch_block_tables(int n_seqs, int B, int b_max, const int32_t* old_
                        pos, status, TabPlan{});
     return hipGetLastError();
   }
-  const TabPlan plan{ws, ws + n_seqs + 1, ws + 2 * (n_seqs + 1)};
-  hipLaunchKernelGGL(block_tables_kernel<true>, dim3(1), dim3(kTabThreads), 0, st, n_seqs, B, b_max,
+  int32_t* head = ws + 2 * (n_seqs + 1);
+  const TabPlan plan{ws, ws + n_seqs + 1, head, head + 2};
+  hipLaunchKernelGGL(block_tables_kernel<true>, dim3(1 + kTabCheck), dim3(kTabThreads), 0, st, n_seqs, B, b_max,
                      old_len, new_len, tables, free_pages, n_free, n_pages, rows, n_slots, slots, cu, pos,
                      status, plan);
 #define SW_SPREAD(LDS)                                                                             \
   hipLaunchKernelGGL(spread_kernel<LDS>, dim3(2048), dim3(256), 0, st, n_seqs, B, b_max, old_len,  \
-                     new_len, tables, free_pages, n_pages, rows, n_slots, slots, cu, plan)
+                     new_len, tables, free_pages, n_free, n_pages, rows, n_slots, slots, cu, pos, status, plan)
   if (n_seqs <= kSpreadLds) SW_SPREAD(true); else SW_SPREAD(false);
 #undef SW_SPREAD
   return hipGetLastError();

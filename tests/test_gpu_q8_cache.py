@@ -477,3 +477,38 @@ def test_binding_refuses_tensors_that_do_not_fit():
             sw.sparse_attn_decode_q8(q, cache, **{**args, **change})
     with pytest.raises(sw.SketchWalkError, match="q of"):
         sw.sparse_attn_decode_q8(q[:, :, :32], cache, **args)
+
+
+@pytest.mark.parametrize("n_slots", [40, 9000])
+@pytest.mark.parametrize("entry", [-1, 600, 1 << 30])
+def test_blocks_given_back_need_a_page(n_slots, entry):
+    """A request that gives back a block without a page (in one launch, and with slots over many
+    workgroups; its block among the first and among the last ones): nothing changes, and no such
+    entry gets onto the stack. Blocks that stay may be without one."""
+    for n, at in ((2, (0, 3)), (3, (1, 90)), (1500, (1499, 0)), (1500, (700, 2))):
+        r = _Requests(n, 16, 100, 600 + n, seed=11)
+        lens = [0] * n
+        lens[at[0]] = 1599 if n < 10 else 40
+        lens[0] = max(lens[0], 70)
+        r.check(lens)
+        page = int(r.d_tables[at])
+        r.d_tables[at] = entry if entry < 600 else entry + n
+        state = (r.d_tables.clone(), r.d_free.clone(), r.d_n.clone())
+        gone = [0 if s == at[0] else x + 1 for s, x in enumerate(lens)]
+        gone = [x if x <= 1600 else 1600 for x in gone]
+        out = sw.block_tables(_i32(lens), _i32(gone), 16, r.d_tables, r.d_free, r.d_n, max(n_slots, n))
+        assert int(out["status"]) == 2
+        assert torch.all(out["slots"] == -1) and torch.all(out["cu"] == 0) and out["pos"].tolist() == [x - 1 for x in lens]
+        for a, b in zip(state, (r.d_tables, r.d_free, r.d_n)):
+            assert torch.equal(a, b)
+        # the request keeps the block: served
+        if at[1] > 0:
+            keep = list(lens)
+            keep[at[0]] = 16 * (at[1] + 1)
+            out = sw.block_tables(_i32(lens), _i32(keep), 16, r.d_tables, r.d_free, r.d_n, max(n_slots, n))
+            assert int(out["status"]) == 0
+            r.lens, r.d_tables[at] = keep, page
+            R.allocate(lens, keep, 16, r.tables, r.stack)
+        else:
+            r.d_tables[at] = page
+        r.check([0] * n, extra=n_slots)              # with its page back, everything goes back
