@@ -402,7 +402,10 @@ int sw_decode_step(int dtype, int layers, int batch, int h_q, int h_kv, int d, i
  * the smallest power of two (at least 2^-126) with which no value exceeds 448,
  * the largest code; a code is x / scale rounded to nearest even, so a stored
  * value is off by at most 2^-4 of itself, or 2^-10 of the scale below 2^-6 of
- * it. A value that is not finite is stored as NaN and does not count for the
+ * it. A larger token that comes to a page later makes the scale larger, and codes
+ * then below 2^-6 of it are rounded again: after any number of such tokens a stored
+ * value is off by at most 2^-4 of itself or 2^-9 of the last scale. A value that is
+ * not finite is stored as NaN and does not count for the
  * scale. Layers are stacked: pages and scales of layer l follow those of layer
  * l - 1, and share one block table.
  *
@@ -425,7 +428,8 @@ int sw_decode_step(int dtype, int layers, int batch, int h_q, int h_kv, int d, i
  * on top of the stack of free pages; their entries become -1. Blocks
  * ceil(old / B) .. ceil(new / B) - 1 of one that enters or grows then take the
  * pages on top, in the same order. Taking a step back therefore restores
- * tables and stack as they were.
+ * tables and stack as they were; a page that stays keeps the scale that a token
+ * taken back has made larger, and its other tokens the rounding to it.
  *
  *   old_len, new_len [n_seqs] int32       tables [n_seqs][b_max] int32, updated
  *   free_pages [n_pages] int32, n_free [1] int32: the stack and its height,

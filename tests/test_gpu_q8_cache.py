@@ -512,3 +512,31 @@ def test_blocks_given_back_need_a_page(n_slots, entry):
         else:
             r.d_tables[at] = page
         r.check([0] * n, extra=n_slots)              # with its page back, everything goes back
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_stored_values_after_their_scale_has_grown(dtype):
+    """A page begun with one of 448 and small ones, then larger tokens one by one: each growth
+    rounds the codes again, and all of them together stay within 2^-4 of the value or 2^-9 of
+    the last scale; within 2^-10 of it while the scale is the first."""
+    h, B, d = 1, 32, 128
+    cache, pool = sw.new_cache_q8(1, h, B, d, U.DEV), R.Pool(1, h, B, d)
+    rng = np.random.default_rng(16)
+    x = np.exp2(rng.uniform(-12, 0, size=(h, 16, d))) * np.sign(rng.normal(size=(h, 16, d)))
+    x[0, 0, 0], x[0, 0, 1] = 448.0, 2.501 * 2.0 ** -9
+    told = torch.from_numpy(x).to(dtype).double().numpy()
+    worst = []
+    for step in range(7):
+        new = told if step == 0 else np.full((h, 1, d), 448.0 * 2.0 ** step)
+        slots = list(range(16)) if step == 0 else [15 + step]
+        t = torch.from_numpy(new).to(dtype).to(U.DEV)
+        sw.kv_append_q8(t, -t, _i32(slots), cache)
+        pool.append(new, -new, slots)
+        _same_cache(cache, pool)
+        scale = 2.0 ** step
+        for n, sign in (("k", 1.0), ("v", -1.0)):
+            err = np.abs(R.cache_values(cache)[0][n][0, :, :16] - sign * told)
+            bound = np.maximum(np.abs(told) * 2.0 ** -4, scale * 2.0 ** (-10 if step == 0 else -9))
+            assert np.all(err <= bound), (step, n)
+            worst.append(float((err / np.maximum(np.abs(told) * 2.0 ** -4, scale * 2.0 ** -10)).max()))
+    assert max(worst[:2]) <= 1.0 < max(worst[2:])    # the second rounding is there
