@@ -404,10 +404,11 @@ int sw_decode_step(int dtype, int layers, int batch, int h_q, int h_kv, int d, i
  * value is off by at most 2^-4 of itself, or 2^-10 of the scale below 2^-6 of
  * it. A larger token that comes to a page later makes the scale larger, and codes
  * then below 2^-6 of it are rounded again: after any number of such tokens a stored
- * value is off by at most 2^-4 of itself or 2^-9 of the last scale. A value that is
- * not finite is stored as NaN and does not count for the
- * scale. Layers are stacked: pages and scales of layer l follow those of layer
- * l - 1, and share one block table.
+ * value is off by at most 2^-4 of itself or 2^-9 of the last scale. Finite values
+ * from 1.9375 * 2^127 in magnitude on are stored as 2^128, which no type of a
+ * caller holds: they read back as infinity. A value that is not finite is stored as
+ * NaN and does not count for the scale. Layers are stacked: pages and scales of layer
+ * l follow those of layer l - 1, and share one block table.
  *
  * Block table of a sequence: tables [n_seqs][b_max] int32, the page of each of
  * its blocks. An entry outside [0, n_pages) is no page: nothing is written
@@ -481,7 +482,7 @@ int sw_kv_append_q8(int dtype, const void* k, const void* v, int64_t k_head_stri
  * first[s] .. of sequence s into rows cu_seqlens[s] .. cu_seqlens[s+1] - 1 of K
  * and V [h_kv][N][d], the layout that sw_sparse_attn_prefill and
  * sw_sketch_scores take (a cached prefix before a longer prompt). The values are
- * exact (in bf16 from 2^-133, its smallest number, on). first [n_seqs] int32 may be
+ * exact (in bf16 from 2^-133, its smallest number, on; below 2^128). first [n_seqs] int32 may be
  * NULL (0), cu_seqlens [n_seqs + 1] int32: both device. A position without a page
  * reads as zero; rows behind the last sequence are left as they were.
  */

@@ -540,3 +540,23 @@ def test_stored_values_after_their_scale_has_grown(dtype):
             assert np.all(err <= bound), (step, n)
             worst.append(float((err / np.maximum(np.abs(told) * 2.0 ** -4, scale * 2.0 ** -10)).max()))
     assert max(worst[:2]) <= 1.0 < max(worst[2:])    # the second rounding is there
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_the_largest_finite_values(dtype):
+    """Below 1.9375 * 2^127 they are stored as finite ones, from there on as 2^128, which reads
+    back as infinity."""
+    h, B, d = 1, 16, 64
+    cache = sw.new_cache_q8(1, h, B, d, U.DEV)
+    edge = 1.9375 * 2.0 ** 127
+    step = 2.0 ** 127 * torch.finfo(dtype).eps
+    vals = [1.0 * 2.0 ** 127, 1.875 * 2.0 ** 127, edge - step, edge, float(torch.finfo(dtype).max)]
+    x = torch.zeros((h, B, d), dtype=torch.float64)
+    x[0, 0, :5] = torch.tensor(vals, dtype=torch.float64)
+    x[0, 1, :5] = -x[0, 0, :5]
+    t = x.to(dtype)
+    assert torch.equal(t.double(), x)
+    sw.kv_append_q8(t.to(U.DEV), t.to(U.DEV), torch.arange(B, dtype=torch.int32, device=U.DEV), cache)
+    for out in sw.kv_fetch_q8(cache, _i32([[0]]), None, _i32([0, B]), B, dtype=dtype):
+        want = torch.tensor([vals[0], vals[1], vals[1], math.inf, math.inf], dtype=torch.float64)
+        assert torch.equal(out[0, 0, :5].double().cpu(), want) and torch.equal(out[0, 1, :5].double().cpu(), -want)
