@@ -504,8 +504,10 @@ int64_t sw_decode_attn_q8_workspace_bytes(int batch, int h_q, int h_kv, int d);
  * selected blocks has a page, get zeros; a head whose tokens' logits are all NaN or
  * -infinity gets NaN.
  * dtype (q, O) SW_BF16 or SW_F32; h_q / h_kv in [1, 16]; any kmax. bf16 takes the
- * weights to 16 bits; fp32 takes q and the weights to 24 bits (queries and values
- * from 2^-80 in magnitude on). Sums are held in fp32. How the work is shared out,
+ * weights to 16 bits; fp32 takes q and the weights to 24 bits. That holds for queries
+ * and values of 2^-80 to 2^90 in magnitude and logits that fp32 holds (smaller ones
+ * may count as 0; larger ones overflow to infinity, or NaN where infinities of both
+ * signs meet). Sums are held in fp32. How the work is shared out,
  * and so the last bits, depend on the call's lengths.
  */
 int sw_sparse_attn_decode_q8(int dtype, const void* q, const void* k_pages, const void* v_pages,

@@ -547,3 +547,20 @@ def test_unlisted_pages_may_have_any_scale(batch, dtype):
         for n in "kv":
             c["cache"][n + "_scale"][rest] = byte
         assert torch.equal(clean, _run(c)), byte
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("q_exp,v_exp", [(-80, 0), (90, 0), (0, -80), (0, 90), (90, 90)])
+def test_queries_and_values_at_the_ends_of_the_range(dtype, q_exp, v_exp):
+    """Magnitudes of 2^-80 and 2^90, with keys that bring the logits back to ordinary ones."""
+    c = _case(29, 2, 8, 2, 128, 64, 600, dtype)
+    c["q"] = (torch.sign(c["q"].float()) * torch.clamp(c["q"].float().abs(), 1.0, 1.99) * 2.0 ** q_exp).to(dtype)
+    c["cache"]["k_scale"] = (c["cache"]["k_scale"].int() - q_exp).to(torch.uint8)
+    if v_exp:
+        # codes of at least 32, so that every value is of the magnitude
+        v = c["cache"]["v"].float()
+        c["cache"]["v"].copy_((torch.sign(v + 0.1) * v.abs().clamp(32, 60)).to(torch.float8_e4m3fn))
+        c["cache"]["v_scale"].fill_(127 + v_exp - 5)
+    got = _run(c)
+    assert torch.isfinite(got).all()
+    _check(c, got)
