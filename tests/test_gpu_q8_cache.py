@@ -1,5 +1,7 @@
 """The paged 8-bit cache on the GPU against its definition: page tables and slots
 exactly, stored values and scales exactly, read-back exactly."""
+import math
+
 import numpy as np
 import pytest
 import torch
