@@ -482,9 +482,10 @@ int sw_kv_append_q8(int dtype, const void* k, const void* v, int64_t k_head_stri
  * first[s] .. of sequence s into rows cu_seqlens[s] .. cu_seqlens[s+1] - 1 of K
  * and V [h_kv][N][d], the layout that sw_sparse_attn_prefill and
  * sw_sketch_scores take (a cached prefix before a longer prompt). The values are
- * exact (in bf16 from 2^-133, its smallest number, on; below 2^128). first [n_seqs] int32 may be
- * NULL (0), cu_seqlens [n_seqs + 1] int32: both device. A position without a page
- * reads as zero; rows behind the last sequence are left as they were.
+ * exact (in bf16 from 2^-133, its smallest number, on; below 2^128).
+ * first [n_seqs] int32 may be NULL (0), cu_seqlens [n_seqs + 1] int32: both device. A
+ * position without a page, a negative one among them, reads as zero; rows behind the
+ * last sequence are left as they were.
  */
 int sw_kv_fetch_q8(int dtype, const void* k_pages, const void* v_pages, const uint8_t* k_scale,
                    const uint8_t* v_scale, int n_pages, int h_kv, int d, int B, int n_seqs, int b_max,

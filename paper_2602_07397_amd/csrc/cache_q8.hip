@@ -740,6 +740,7 @@ hipError_t launch_kv_append_q8(int dtype, int layers, const void* k, const void*
 // ---------------------------------------------------------------------------
 
 constexpr int kFetchTile = 64;                     // positions per workgroup, four chunks of 16
+static_assert(kFetchTile == 1 << 6, "positions are shifted");
 constexpr int kFetchStride = kFetchTile + 4;       // bytes from one dimension's row to the next in LDS
 
 // One workgroup per (64 positions of a sequence, head): positions first[s] ..
@@ -771,14 +772,15 @@ __global__ __launch_bounds__(256) void kv_fetch_q8_kernel(
   int s, c0, c1;
   const long long u = seq_of_wg(wg, n_seqs, cu, kFetchTile, N, &s, &c0, &c1);
   if (c0 >= c1 || u < 0) return;
-  const int p0 = first ? max(first[s], 0) : 0;
-  const long long pt = (p0 / kFetchTile + u) * kFetchTile;   // the tile's first position
+  const int p0 = first ? first[s] : 0;
+  const long long pt = ((p0 >> 6) + u) * kFetchTile;   // the tile's first position (p0 may be negative)
   // places lo .. hi - 1 of the tile are asked for; place o is row row0 + o
   const long long row0 = c0 + pt - p0;
   const int lo = (int)max(0ll, c0 - row0), hi = (int)min((long long)kFetchTile, c1 - row0);
   if (lo >= hi) return;
   // page and head of each chunk (-1 without a page) and its place in the page
   if (t < 4) {
+    // a negative position is 2^31 or more here, behind every table
     const uint32_t p = (uint32_t)pt + 16 * t, j = p / (uint32_t)B;
     const int page = j < (uint32_t)b_max && pt < (1ll << 31) ? tables[(long long)s * b_max + j] : -1;
     at4[t] = (unsigned)page < (unsigned)n_pages ? (long long)page * h_kv + g : -1ll;

@@ -562,3 +562,25 @@ def test_the_largest_finite_values(dtype):
     for out in sw.kv_fetch_q8(cache, _i32([[0]]), None, _i32([0, B]), B, dtype=dtype):
         want = torch.tensor([vals[0], vals[1], vals[1], math.inf, math.inf], dtype=torch.float64)
         assert torch.equal(out[0, 0, :5].double().cpu(), want) and torch.equal(out[0, 1, :5].double().cpu(), -want)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_fetch_from_before_the_first_position(dtype):
+    """Negative positions have no page: their rows are zero, those behind them keep their places."""
+    rng = np.random.default_rng(17)
+    h, B, d, P = 2, 16, 64, 30
+    cache = _filled(rng, P, h, B, d)
+    first, lens = [-1, -70, -64, -200, -(1 << 31), 3], [40, 150, 64, 100, 70, 5]
+    tables = rng.permutation(P).reshape(6, 5).astype(np.int32)
+    cu = [0] + np.cumsum(lens).tolist()
+    K, V = sw.kv_fetch_q8(cache, U.to_dev(tables), _i32(first), _i32(cu), cu[-1], dtype=dtype)
+    pool = R.Pool(P, h, B, d)
+    pool.x, _ = R.cache_values(cache)
+    for got, n in ((K, "k"), (V, "v")):
+        got = got.cpu().double().numpy()
+        for s, (a, m) in enumerate(zip(first, lens)):
+            want = np.zeros((h, m, d))
+            at = [i for i in range(m) if a + i >= 0]
+            if at:
+                want[:, at] = pool.tokens(n, tables[s], [a + i for i in at])
+            np.testing.assert_array_equal(got[:, cu[s]:cu[s + 1]], want)
