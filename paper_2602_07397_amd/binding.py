@@ -668,13 +668,18 @@ def kv_append_q8(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache: d
 
 
 def kv_fetch_q8(cache: dict, tables: torch.Tensor, first: Optional[torch.Tensor], cu: torch.Tensor, N: int,
-                dtype: torch.dtype = torch.bfloat16, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None):
-    """K, V [h_kv][N][d] in ``dtype``: positions first[s] .. (``first`` None: 0) of sequence
-    s in rows cu[s] .. cu[s + 1] - 1 (device int32). Rows behind cu[n] are not written."""
+                dtype: Optional[torch.dtype] = None, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None):
+    """K, V [h_kv][N][d] in ``dtype`` (None: that of ``out``, bf16 without): positions first[s] ..
+    (``first`` None: 0) of sequence s in rows cu[s] .. cu[s + 1] - 1 (device int32). Rows
+    behind cu[n] are not written."""
     ck = cache["k"]
+    K, V = (None, None) if out is None else out
+    if dtype is None:
+        dtype = torch.bfloat16 if K is None else K.dtype
+    elif K is not None and K.dtype is not dtype:
+        raise SketchWalkError(f"out has dtype {K.dtype}, not {dtype}")
     if dtype is not torch.bfloat16 and dtype is not torch.float32:
         raise SketchWalkError(f"unsupported dtype {dtype}")
-    K, V = (None, None) if out is None else out
     return _native("kv_fetch_q8", ck, ck, cache["v"], cache["k_scale"], cache["v_scale"], tables, first, cu, N,
                    SW_BF16 if dtype is torch.bfloat16 else SW_F32, K, V)
 

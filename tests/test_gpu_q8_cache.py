@@ -584,3 +584,18 @@ def test_fetch_from_before_the_first_position(dtype):
             if at:
                 want[:, at] = pool.tokens(n, tables[s], [a + i for i in at])
             np.testing.assert_array_equal(got[:, cu[s]:cu[s + 1]], want)
+
+
+def test_fetch_into_tensors_of_another_type_is_refused():
+    cache = sw.new_cache_q8(2, 1, 16, 64, U.DEV)
+    args = (cache, _i32([[0]]), None, _i32([0, 4]), 4)
+    for own, other in ((torch.float32, torch.bfloat16), (torch.bfloat16, torch.float32)):
+        out = tuple(torch.ones((1, 4, 64), dtype=own, device=U.DEV) for _ in range(2))
+        with pytest.raises(sw.SketchWalkError, match="dtype"):
+            sw.kv_fetch_q8(*args, dtype=other, out=out)
+        for kw in ({}, {"dtype": own}):              # out's own type, named or not
+            K, V = sw.kv_fetch_q8(*args, out=out, **kw)
+            assert K.dtype is own and torch.all(K == 0) and torch.all(V == 0)
+            K.fill_(1)
+            V.fill_(1)
+    assert sw.kv_fetch_q8(*args)[0].dtype is torch.bfloat16
