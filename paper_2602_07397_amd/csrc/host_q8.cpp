@@ -65,6 +65,12 @@ int32_t* ints(const at::Tensor& t, int64_t n, int64_t di, const char* name) {
 
 int32_t* ints(PyObject* o, int64_t n, int64_t di, const char* name) { return ints(tensor(o, name), n, di, name); }
 
+// A size that the C ABI takes as int.
+int fits(int64_t n, const char* what) {
+  if (n > INT32_MAX) throw Refused(std::string(what) + ": " + std::to_string(n) + " does not fit in 32 bits");
+  return (int)n;
+}
+
 void shaped(const at::Tensor& t, at::IntArrayRef want, const char* name) {
   if (t.sizes() == want) return;
   std::string s = std::string(name) + " of shape " + shape_of(t) + ", (";
@@ -124,14 +130,13 @@ struct Pool {
 Pool pool_of(PyObject* const* a, int64_t di) {
   const at::Tensor &k = tensor(a[0], "cache k"), &v = tensor(a[1], "cache v"), &ks = tensor(a[2], "cache k_scale"),
                    &vs = tensor(a[3], "cache v_scale");
-  const bool fits = k.dim() == 4 && v.dim() == 4 && ks.dim() == 2 && v.size(0) == k.size(0) && v.size(1) == k.size(1) &&
+  const bool same = k.dim() == 4 && v.dim() == 4 && ks.dim() == 2 && v.size(0) == k.size(0) && v.size(1) == k.size(1) &&
                     v.size(2) == k.size(3) && v.size(3) == k.size(2) && ks.size(0) == k.size(0) &&
                     ks.size(1) == k.size(1) && vs.sizes() == ks.sizes();
-  if (!fits)
+  if (!same)
     throw Refused("cache of shapes k " + shape_of(k) + ", v " + shape_of(v) + ", k_scale " + shape_of(ks) + ", v_scale " +
                   shape_of(vs) + ": (n_pages, h_kv, B, d), (n_pages, h_kv, d, B) and twice (n_pages, h_kv) needed");
-  if (k.size(0) > INT32_MAX) throw Refused("cache k has too many pages");
-  return {(int)k.size(0), (int)k.size(1), (int)k.size(2), (int)k.size(3),
+  return {fits(k.size(0), "pages"), fits(k.size(1), "h_kv"), fits(k.size(2), "B"), fits(k.size(3), "d"),
           address(k, at::kFloat8_e4m3fn, di, "cache k"), address(v, at::kFloat8_e4m3fn, di, "cache v"),
           static_cast<uint8_t*>(address(ks, at::kByte, di, "cache k_scale")),
           static_cast<uint8_t*>(address(vs, at::kByte, di, "cache v_scale"))};
@@ -148,31 +153,33 @@ PyObject* block_tables(PyObject* const* a, Py_ssize_t n_args) {
   const int64_t di = integer(a[0], "device");
   const at::Tensor &old = tensor(a[2], "old_len"), &tables = tensor(a[5], "tables"), &pages = tensor(a[6], "free_pages");
   if (tables.dim() != 2) throw Refused("tables of shape " + shape_of(tables) + ", (n, b_max) needed");
-  const int64_t n = tables.size(0), n_slots = integer(a[8], "n_slots");
+  const int64_t n_slots = integer(a[8], "n_slots");
+  const int n = fits(tables.size(0), "requests"), b_max = fits(tables.size(1), "b_max"),
+            n_pages = fits(pages.numel(), "free_pages");
   void* p_old = ints(old, n, di, "old_len");
-  const int64_t wsb = p_block_tables_ws((int)n, n_slots);
+  const int64_t wsb = p_block_tables_ws(n, n_slots);
   if (wsb < 0) check(SW_ERR_INVALID_ARG, "sw_block_tables_workspace_bytes");
   const at::Tensor slots = out_or(a[10], old, n_slots, at::kInt, "slots");
   at::Tensor cu, pos, status, ws;
   if (a[11] == Py_None && a[12] == Py_None && a[13] == Py_None) {
     // the small outputs together, in 64-byte pieces: an allocation takes 0.7 us on the host
-    const int64_t c = (n + 16) & ~15ll, p = (n + 15) & ~15ll;
+    const int64_t c = (n + 16ll) & ~15ll, p = (n + 15ll) & ~15ll;
     const at::Tensor all = at::empty({c + p + 1}, old.options().dtype(at::kInt));
-    cu = piece(all, 0, n + 1);
+    cu = piece(all, 0, n + 1ll);
     pos = piece(all, c, n);
     status = piece(all, c + p, 1);
   } else {
-    cu = out_or(a[11], old, n + 1, at::kInt, "cu");
+    cu = out_or(a[11], old, n + 1ll, at::kInt, "cu");
     pos = out_or(a[12], old, n, at::kInt, "pos");
     status = out_or(a[13], old, 1, at::kInt, "status");
   }
   if (a[14] != Py_None) ws = tensor(a[14], "workspace");
   if (wsb > 0 && (!ws.defined() || ws.numel() < wsb)) ws = at::empty({wsb}, old.options().dtype(at::kByte));
-  check(p_block_tables((int)n, small(a[4], "B"), (int)tables.size(1), static_cast<int32_t*>(p_old),
+  check(p_block_tables(n, small(a[4], "B"), b_max, static_cast<int32_t*>(p_old),
                        ints(a[3], n, di, "new_len"), static_cast<int32_t*>(address(tables, at::kInt, di, "tables")),
                        static_cast<int32_t*>(address(pages, at::kInt, di, "free_pages")), ints(a[7], 1, di, "n_free"),
-                       (int)pages.numel(), small(a[9], "rows"), n_slots, ints(slots, n_slots, di, "slots"),
-                       ints(cu, n + 1, di, "cu"), ints(pos, n, di, "pos"), ints(status, 1, di, "status"),
+                       n_pages, small(a[9], "rows"), n_slots, ints(slots, n_slots, di, "slots"),
+                       ints(cu, n + 1ll, di, "cu"), ints(pos, n, di, "pos"), ints(status, 1, di, "status"),
                        ws.defined() ? address(ws, at::kByte, di, "workspace") : nullptr,
                        ws.defined() ? ws.numel() : 0, stream_of(a[1])),
         "sw_block_tables");
@@ -213,14 +220,14 @@ PyObject* kv_append_q8(PyObject* const* a, Py_ssize_t n_args) {
 PyObject* kv_fetch_q8(PyObject* const* a, Py_ssize_t n_args) {
   count(n_args, 13);
   const int64_t di = integer(a[0], "device"), N = integer(a[9], "N");
-  const Pool c = pool_of(a + 2, di);
   const at::Tensor& tables = tensor(a[6], "tables");
   if (tables.dim() != 2) throw Refused("tables of shape " + shape_of(tables) + ", (n, b_max) needed");
+  const int n = fits(tables.size(0), "sequences"), b_max = fits(tables.size(1), "b_max");
+  const Pool c = pool_of(a + 2, di);
   if (N < 0) throw Refused("N=" + std::to_string(N) + " < 0");
-  const int64_t n = tables.size(0);
   void* p_tables = address(tables, at::kInt, di, "tables");
   const int32_t* p_first = a[7] == Py_None ? nullptr : ints(a[7], n, di, "first");
-  const int32_t* p_cu = ints(a[8], n + 1, di, "cu");
+  const int32_t* p_cu = ints(a[8], n + 1ll, di, "cu");
   at::Tensor K, V;
   if (a[11] == Py_None) {
     const auto type = integer(a[10], "dtype") == SW_BF16 ? at::kBFloat16 : at::kFloat;
@@ -233,7 +240,7 @@ PyObject* kv_fetch_q8(PyObject* const* a, Py_ssize_t n_args) {
     shaped(V, {c.h_kv, N, c.d}, "V");
   }
   const auto type = K.scalar_type();
-  check(p_fetch(type_code(K), c.k, c.v, c.ks, c.vs, c.n_pages, c.h_kv, c.d, c.B, (int)n, (int)tables.size(1),
+  check(p_fetch(type_code(K), c.k, c.v, c.ks, c.vs, c.n_pages, c.h_kv, c.d, c.B, n, b_max,
                 static_cast<int32_t*>(p_tables), p_first, p_cu, N, address(K, type, di, "K"), address(V, type, di, "V"),
                 stream_of(a[1])),
         "sw_kv_fetch_q8");
@@ -246,11 +253,11 @@ PyObject* sparse_attn_decode_q8(PyObject* const* a, Py_ssize_t n_args) {
   count(n_args, 15);
   const int64_t di = integer(a[0], "device");
   const at::Tensor &q = tensor(a[2], "q"), &tables = tensor(a[7], "tables"), &idx = tensor(a[9], "idx");
+  const int b_max = tables.dim() == 2 ? fits(tables.size(1), "b_max") : 0;
   const Pool c = pool_of(a + 3, di);
   if (q.dim() != 3 || q.size(2) != c.d)
     throw Refused("q of shape " + shape_of(q) + ", (batch, h_q, " + std::to_string(c.d) + ") needed");
-  const int64_t batch = q.size(0), h_q = q.size(1);
-  if (batch > INT32_MAX || h_q > INT32_MAX) throw Refused("q of shape " + shape_of(q) + " is too large");
+  const int batch = fits(q.size(0), "batch"), h_q = fits(q.size(1), "h_q");
   if (tables.dim() != 2 || tables.size(0) != batch)
     throw Refused("tables of shape " + shape_of(tables) + ", (" + std::to_string(batch) + ", b_max) needed");
   const int kmax = small(a[11], "kmax");
@@ -263,7 +270,7 @@ PyObject* sparse_attn_decode_q8(PyObject* const* a, Py_ssize_t n_args) {
     PyErr_Clear();
     throw Refused("scale must be a number");
   }
-  const int64_t wsb = p_attn_ws((int)batch, (int)h_q, c.h_kv, c.d);
+  const int64_t wsb = p_attn_ws(batch, h_q, c.h_kv, c.d);
   if (wsb < 0) check(SW_ERR_INVALID_ARG, "sw_decode_attn_q8_workspace_bytes");
   at::Tensor O, ws;
   if (a[13] == Py_None) {
@@ -274,8 +281,8 @@ PyObject* sparse_attn_decode_q8(PyObject* const* a, Py_ssize_t n_args) {
   }
   if (a[14] != Py_None) ws = tensor(a[14], "workspace");
   if (wsb > 0 && (!ws.defined() || ws.numel() < wsb)) ws = at::empty({wsb}, q.options().dtype(at::kByte));
-  check(p_attn(code, p_q, c.k, c.v, c.ks, c.vs, (int)batch, (int)h_q, c.h_kv, c.d, c.n_pages,
-               static_cast<int32_t*>(address(tables, at::kInt, di, "tables")), (int)tables.size(1), c.B,
+  check(p_attn(code, p_q, c.k, c.v, c.ks, c.vs, batch, h_q, c.h_kv, c.d, c.n_pages,
+               static_cast<int32_t*>(address(tables, at::kInt, di, "tables")), b_max, c.B,
                ints(a[8], batch, di, "pos"), static_cast<int32_t*>(address(idx, at::kInt, di, "idx")),
                ints(a[10], batch, di, "cnt"), kmax, (float)scale, address(O, type, di, "O"),
                ws.defined() ? address(ws, at::kByte, di, "workspace") : nullptr, ws.defined() ? ws.numel() : 0,

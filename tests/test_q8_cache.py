@@ -156,3 +156,26 @@ def test_binding_refuses_what_does_not_fit():
         sw.block_tables(i32, i32, 16, torch.zeros((4, 2), dtype=torch.int32), i32, i32[:1], 4.5)
     with pytest.raises(sw.SketchWalkError, match="dtype"):
         sw.kv_fetch_q8(cache, i32[None], None, i32[:2], 4, dtype=torch.float16)
+
+
+def test_binding_refuses_sizes_that_do_not_fit_in_32_bits():
+    """They are not cut to 32 bits (views of one entry; refused before anything else is looked at)."""
+    cache = sw.new_cache_q8(4, 2, 16, 64, "cpu")
+    i32 = torch.zeros(4, dtype=torch.int32)
+    one = torch.zeros((1, 1), dtype=torch.int32)
+    far = (1 << 32) + 5                              # 5 in the lower 32 bits
+    tables = torch.zeros((4, 2), dtype=torch.int32)
+    for args in ((i32, i32, 16, tables, one[0].expand(far), i32[:1], 4),
+                 (i32, i32, 16, one.expand(4, far), i32, i32[:1], 4),
+                 (one[0].expand(far), one[0].expand(far), 16, one.expand(far, 2), i32, i32[:1], 4)):
+        with pytest.raises(sw.SketchWalkError, match="32 bits"):
+            sw.block_tables(*args)
+    for t in (one.expand(far, 2), one.expand(4, far)):
+        with pytest.raises(sw.SketchWalkError, match="32 bits"):
+            sw.kv_fetch_q8(cache, t, None, i32, 4)
+    with pytest.raises(sw.SketchWalkError, match="32 bits"):
+        sw.sparse_attn_decode_q8(torch.zeros((1, 4, 64)), cache, one.expand(1, far), i32[:1], i32[None], i32[:1], 4)
+    with pytest.raises(sw.SketchWalkError, match="32 bits"):
+        sw.kv_append_q8(torch.zeros((2, 4, 64)), torch.zeros((2, 4, 64)), i32, {
+            **cache, "k": cache["k"][:, :1].expand(4, far, 16, 64), "v": cache["v"][:, :1].expand(4, far, 64, 16),
+            "k_scale": cache["k_scale"][:, :1].expand(4, far), "v_scale": cache["v_scale"][:, :1].expand(4, far)})
