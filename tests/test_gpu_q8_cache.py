@@ -599,3 +599,38 @@ def test_fetch_into_tensors_of_another_type_is_refused():
             K.fill_(1)
             V.fill_(1)
     assert sw.kv_fetch_q8(*args)[0].dtype is torch.bfloat16
+
+
+def test_tables_with_many_slots_captured_and_refused_in_between():
+    """A captured call of two launches: served, refused for a block without a page, served again."""
+    r = _Requests(3, 16, 400, 1500, seed=12)
+    r.check([5000, 16, 0])
+    old, new = _i32(r.lens), _i32(r.lens)
+    out = {"slots": _i32([0] * 9000), "cu": _i32([0] * 4), "pos": _i32([0] * 3), "status": _i32([5])}
+    ws = torch.full((sw.load().sw_block_tables_workspace_bytes(3, 9000),), 255, dtype=torch.uint8, device=U.DEV)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        sw.block_tables(old, new, 16, r.d_tables, r.d_free, r.d_n, 9000, out=dict(out), workspace=ws)
+    for target in ([100, 6400, 6], [6400, 0, 2000], [0, 0, 0], [6400, 17, 1]):
+        old.copy_(_i32(r.lens))
+        new.copy_(_i32(target))
+        shrinks = [s for s in range(3) if target[s] // 16 + 1 < r.lens[s] // 16]
+        if shrinks:
+            at = (shrinks[0], r.lens[shrinks[0]] // 16 - 1)
+            page = int(r.d_tables[at])
+            r.d_tables[at] = -1
+            state = (r.d_tables.clone(), r.d_free.clone(), r.d_n.clone())
+            g.replay()
+            assert int(out["status"]) == 2 and torch.all(out["slots"] == -1) and torch.all(out["cu"] == 0)
+            assert out["pos"].tolist() == [x - 1 for x in r.lens]
+            for a, b in zip(state, (r.d_tables, r.d_free, r.d_n)):
+                assert torch.equal(a, b)
+            r.d_tables[at] = page
+        g.replay()
+        slots, cu, pos = R.allocate(r.lens, target, 16, r.tables, r.stack, 0, 9000)
+        assert int(out["status"]) == 0 and out["slots"].tolist() == slots and out["cu"].tolist() == cu
+        assert out["pos"].tolist() == pos and r.d_tables.tolist() == r.tables and r.d_n.tolist() == [len(r.stack)]
+        assert r.d_free[:len(r.stack)].tolist() == r.stack
+        r.lens = list(target)
+        torch.cuda.synchronize()
