@@ -438,7 +438,8 @@ int sw_decode_step(int dtype, int layers, int batch, int h_q, int h_kv, int d, i
  *   slots [n_slots] int32 (out): page * B + place of every new token, requests in
  *     order. rows = 0: packed, -1 behind the last. rows > 0: rows entries per
  *     request (n_slots = n_seqs * rows), -1 behind its new tokens.
- *   cu_seqlens [n_seqs + 1] int32 (out): cumulative numbers of new tokens
+ *   cu_seqlens [n_seqs + 1] int32 (out): cumulative numbers of new tokens, the places
+ *     of a request's slots where they are packed (padded slots go to an append without it)
  *   pos [n_seqs] int32 (out): position of the last token, new_len - 1
  *   status [1] int32 (out): 0; 1: too few free pages; 2: a length outside
  *     [0, b_max * B], more new tokens than slots or than rows, a block given back
@@ -509,7 +510,9 @@ int64_t sw_decode_attn_q8_workspace_bytes(int batch, int h_q, int h_kv, int d);
  * and values of 2^-80 to 2^90 in magnitude and logits that fp32 holds (smaller ones
  * may count as 0; larger ones overflow to infinity, or NaN where infinities of both
  * signs meet). Sums are held in fp32. How the work is shared out,
- * and so the last bits, depend on the call's lengths.
+ * and so the last bits, depend on the call's lengths. The parts of long sequences are
+ * shared out in batches of up to 256; above, one workgroup has each (sequence, KV
+ * head), which takes as long as the longest of them.
  */
 int sw_sparse_attn_decode_q8(int dtype, const void* q, const void* k_pages, const void* v_pages,
                              const uint8_t* k_scale, const uint8_t* v_scale, int batch, int h_q,

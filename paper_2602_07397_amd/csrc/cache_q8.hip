@@ -132,7 +132,7 @@ __device__ __forceinline__ bool without_page(int wave, int waves, int n_seqs, in
 // blocks ascending) is on top, and the A new blocks take pages from the top in the
 // same order. Bounded by latency, three to five dependent loads and as many
 // barriers: 4.6 us for one token more for each of 64 requests. PLAN: the prefixes
-// alone, for spread_kernel (3.4 us for 512 requests): pages moved by one workgroup
+// alone, for spread_kernel (4.3 us for 512 requests): pages moved by one workgroup
 // take 1.5 us per 1024, slots as much. A block given back has to have a page: the
 // workgroup looks at them itself where there are any (64 requests, a step of one token and the
 // same step back in turn: 4.6 -> 5.0 us a call); PLAN: kTabCheck workgroups beside it, and
@@ -275,7 +275,7 @@ constexpr int kSpreadLds = 1024;                   // sequences whose lengths an
 // stack where there is none: no workgroup reads what another one writes. Slots of
 // the blocks that the sequences had before, and those that stay empty, are
 // written per sequence and behind the last. 512 requests, a third of them prompts of
-// 20000 tokens at most: 27000 pages and 1.7 million slots in 7.1 us, 52 with both by
+// 20000 tokens at most: 27000 pages and 1.7 million slots in 6.8 us, 52 with both by
 // one workgroup and a search per slot. Eight workgroups per CU, as many as run at once
 // (four: 7.9 us; sixteen: 7.2).
 template <bool LDS>
